@@ -535,6 +535,151 @@ hcmix_status hcmix_head_cross_entropy(int64_t rows, int64_t width, int32_t vocab
                                       float scale, float* loss, void* dlogits, float* dbias,
                                       void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Attention layers past the fixed windows: rotary positions, attention over
+ * any length with shared key/value heads, and an 8-bit key/value cache ----
+ *
+ * Activations are [batch][n][heads][head_dim]: a position's heads lie side by
+ * side, and consecutive positions of the whole batch lie `stride` elements
+ * apart (stride >= heads * head_dim; sequence b's position i is row b * n + i),
+ * so that the queries, keys and values of one packed projection can be given
+ * where they are.  Extents count the elements that are touched: an output may
+ * lie between the rows of an input or of another output, with the same stride.
+ */
+
+/* Rotary positions.  With t = position * freqs[j], the pair j of every head,
+ *   (a, b) = (x[j], x[j + rot_dim / 2])   HCMIX_ROTARY_HALF
+ *   (a, b) = (x[2j], x[2j + 1])           HCMIX_ROTARY_PAIRS,
+ * becomes scale * (a cos t - b sin t, b cos t + a sin t); the values from rot_dim
+ * on are copied.  inverse != 0 takes -t: the transpose, hence the backward (with
+ * the forward's scale).
+ *   x, y: `rows` rows of heads * head_dim values in dtype, x_stride and y_stride
+ *     apart; y is x (same stride: in place) or overlaps it nowhere.
+ *   positions: int32 [rows] (any sign), or NULL: row r stands at r % period.
+ *   freqs: fp64 [rot_dim / 2], radians per position, device memory.
+ * Angles are taken in 64 bits and reduced there, products and sums in 32 bits,
+ * outputs rounded once.  head_dim and rot_dim even, rot_dim <= head_dim <= 512,
+ * heads <= 1024, rows <= 2^30.
+ * HCMIX_ERR_INVALID_VALUE: null pointers, sizes or period < 1, sizes past those
+ * bounds, strides below heads * head_dim, an unknown layout or dtype, a scale
+ * that is not finite, overlaps.  HCMIX_ERR_UNSUPPORTED: an odd head_dim or
+ * rot_dim, pointers not aligned to an element (freqs: 8 bytes). */
+enum { HCMIX_ROTARY_HALF = 0, HCMIX_ROTARY_PAIRS = 1 };
+
+hcmix_status hcmix_rotary(int64_t rows, int32_t heads, int32_t head_dim, int32_t rot_dim,
+                          int32_t layout, int32_t inverse, int32_t dtype, const void* x,
+                          int64_t x_stride, const int32_t* positions, int64_t period,
+                          const double* freqs, float scale, void* y, int64_t y_stride,
+                          void* stream);
+
+/* Attention of n_q queries over n_k keys per sequence, q_heads query heads in
+ * groups of q_heads / kv_heads that share a key/value head (query head h takes
+ * key/value head h / group):
+ *   S[i][j] = scale q_i . k_j,  P = row softmax of S over the keys seen,  out = P v,
+ *   lse[i] = ln sum_j exp(S[i][j]).
+ * Query i sees key j when j < lengths[b] (int32 [batch], taken within 0 .. n_k;
+ * NULL: n_k) and, causal != 0, j <= i + n_k - n_q (the last query stands at the
+ * last key).  A row that sees nothing gets out = 0 and lse = -inf, and gives no
+ * gradient.  What keys and values from lengths[b] on hold is never taken.
+ *   q, k, v: bf16 as above, head_dim 64 or 128; out: bf16 [batch][n_q][q_heads]
+ *   [head_dim], lse: fp32 [batch][q_heads][n_q], both contiguous.
+ * Precision: products of bf16 with fp32 accumulation, softmax statistics in fp32,
+ * P (and the backward's P and dS) rounded to bf16 for the second products.
+ * n_q, n_k <= 2^20, q_heads <= 1024, batch * n <= 2^30; scale positive, finite.
+ * HCMIX_ERR_INVALID_VALUE: null pointers (lengths may be), sizes < 1 or past
+ * those bounds, q_heads no multiple of kv_heads, causal not 0 or 1, a scale that
+ * is not positive and finite, strides below heads * head_dim, overlaps.
+ * HCMIX_ERR_UNSUPPORTED: another head_dim, strides that are no multiple of 8,
+ * bf16 pointers not 16-byte, others not 4-byte aligned. */
+hcmix_status hcmix_grouped_attention_forward(
+    int64_t batch, int64_t n_q, int64_t n_k, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+    int32_t causal, float scale, const int32_t* lengths, const void* q, int64_t q_stride,
+    const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* out, float* lse,
+    void* stream);
+
+/* Backward: dq, dk, dv (bf16, strides of their own) from the forward's operands,
+ * its out and lse, and dout = dL/dout (contiguous like out):
+ *   dv = P^T dout, dS = P * (dout v^T - rowsum(dout * out)) scale,
+ *   dq = dS k, dk = dS^T q, summed over the query heads of a group.
+ * P is made again from lse.  Sums run in a fixed order (bitwise-repeatable).
+ * dk and dv are 0 from lengths[b] on.  Workspace of the size the query names
+ * (0 for invalid arguments), 256-byte aligned; other errors as above. */
+size_t hcmix_grouped_attention_backward_workspace_bytes(int64_t batch, int64_t n_q, int64_t n_k,
+                                                        int32_t q_heads, int32_t kv_heads,
+                                                        int32_t head_dim);
+
+hcmix_status hcmix_grouped_attention_backward(
+    int64_t batch, int64_t n_q, int64_t n_k, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+    int32_t causal, float scale, const int32_t* lengths, const void* q, int64_t q_stride,
+    const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* out,
+    const float* lse, const void* dout, void* dq, int64_t dq_stride, void* dk, int64_t dk_stride,
+    void* dv, int64_t dv_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Key/value cache in 8 bits: caller-owned device memory of hcmix_kv_cache_bytes()
+ * bytes, 256-byte aligned, for `capacity` tokens of every sequence.  Tokens lie in
+ * blocks of 64; a block holds each head's keys as e4m3 numbers (4 significant
+ * bits, largest 448) times one power of two, and its values likewise: the least
+ * from 2^-118 to 2^120 by which the block's largest magnitude is at most 448.
+ * The layout inside is the library's own.  The cache needs no initialisation:
+ * nothing is taken that was not appended.
+ *
+ * Append: `tokens` tokens of every sequence, k and v bf16 as above, those of
+ * sequence b at positions[b] and behind, its first counts[b] alone (int32
+ * [batch], taken within 0 .. tokens; NULL: all).  What a sequence holds from
+ * positions[b] on is dropped first (so drafted tokens are taken back by
+ * appending at an earlier position).  A block's scale is the larger of what its
+ * new tokens need and, where it keeps earlier ones, its own; earlier ones are
+ * then held again at the new scale.  Tokens at capacity and behind, and those of
+ * a sequence whose positions[b] lies outside 0 .. capacity - 1, are left out.
+ * An infinity takes the scale to 2^120 and is held as 448 times it; NaN is held
+ * as NaN and does not count for the scale.
+ *
+ * Read: k and v (bf16 [batch][tokens][kv_heads][head_dim]) of tokens first[b] ..
+ * first[b] + tokens - 1, the values held (exact in bf16), 0 outside 0 ..
+ * lengths[b] - 1.
+ *
+ * Attention: `tokens` queries of every sequence, the last standing at its last
+ * token: query t at position lengths[b] - tokens + t sees the tokens up to its
+ * own.  q bf16 [batch][tokens][q_heads][head_dim], rows q_stride apart; out bf16,
+ * contiguous; softmax, groups and precision as for hcmix_grouped_attention, keys
+ * and values exact.  A query before the first token gets 0.  lengths: int32
+ * [batch], taken within 0 .. capacity.  max_length (1 .. capacity) says how long
+ * sequences are expected to be: long ones are split over the chip by it (joined
+ * through the workspace of hcmix_kv_cache_attention_workspace_bytes, possibly 0),
+ * and longer ones than it are still right.
+ *
+ * All of positions, counts, first and lengths are device memory, so that a
+ * captured graph can be replayed with other values in them.
+ * HCMIX_ERR_INVALID_VALUE: null pointers (counts may be), sizes < 1, batch above
+ * 65535, capacity above 2^24, tokens above 2^16, heads above 1024, q_heads no
+ * multiple of kv_heads, a cache shorter than the query, a scale that is not
+ * positive and finite, strides below heads * head_dim, overlaps.
+ * HCMIX_ERR_UNSUPPORTED: head_dim not 64 or 128, strides that are no multiple of
+ * 8, bf16 pointers not 16-byte, the cache and workspace not 256-byte, others not
+ * 4-byte aligned. */
+size_t hcmix_kv_cache_bytes(int64_t batch, int64_t capacity, int32_t kv_heads, int32_t head_dim);
+
+hcmix_status hcmix_kv_cache_append(int64_t batch, int64_t capacity, int32_t kv_heads,
+                                   int32_t head_dim, int64_t tokens, const void* k,
+                                   int64_t k_stride, const void* v, int64_t v_stride,
+                                   const int32_t* positions, const int32_t* counts, void* cache,
+                                   size_t cache_bytes, void* stream);
+
+hcmix_status hcmix_kv_cache_read(int64_t batch, int64_t capacity, int32_t kv_heads,
+                                 int32_t head_dim, int64_t tokens, const int32_t* first,
+                                 const int32_t* lengths, const void* cache, size_t cache_bytes,
+                                 void* k, void* v, void* stream);
+
+size_t hcmix_kv_cache_attention_workspace_bytes(int64_t batch, int64_t capacity, int32_t q_heads,
+                                                int32_t kv_heads, int32_t head_dim, int64_t tokens,
+                                                int64_t max_length);
+
+hcmix_status hcmix_kv_cache_attention(int64_t batch, int64_t capacity, int32_t q_heads,
+                                      int32_t kv_heads, int32_t head_dim, int64_t tokens,
+                                      float scale, const void* q, int64_t q_stride,
+                                      const int32_t* lengths, int64_t max_length,
+                                      const void* cache, size_t cache_bytes, void* out,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

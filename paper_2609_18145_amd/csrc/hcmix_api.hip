@@ -1426,3 +1426,402 @@ hcmix_status hcmix_field_backward(int64_t batch, int64_t n, int64_t width, int32
                                   (int)width, 1.f / tau, scaled, (hipStream_t)stream);
   return e == hipSuccess ? HCMIX_OK : hip_fail(e);
 }
+
+// ---- attention layers past the fixed windows ----
+
+namespace {
+
+// An operand of rows that lie `stride` bytes apart, `width` bytes of each touched.
+struct Rows {
+  const void* p;
+  size_t rows, stride, width;
+};
+
+// Whether two of them touch the same byte: with one stride, rows between rows
+// do not.
+bool rows_overlap(const Rows& a, const Rows& b) {
+  const size_t na = (a.rows - 1) * a.stride + a.width, nb = (b.rows - 1) * b.stride + b.width;
+  if (!overlaps(a.p, na, b.p, nb)) return false;
+  if (a.stride != b.stride || a.rows == 1 || b.rows == 1) return true;
+  const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
+  const size_t off = pb >= pa ? (pb - pa) % a.stride : (a.stride - (pa - pb) % a.stride) % a.stride;
+  return off < a.width || off + b.width > a.stride;
+}
+
+// Inputs and outputs as check_spans has them, in rows.
+hcmix_status check_rows(const Rows* ins, int nin, const Rows* outs, int nout) {
+  for (int i = 0; i < nout; i++) {
+    for (int j = 0; j < nin; j++)
+      if (rows_overlap(outs[i], ins[j])) return HCMIX_ERR_INVALID_VALUE;
+    for (int j = i + 1; j < nout; j++)
+      if (rows_overlap(outs[i], outs[j])) return HCMIX_ERR_INVALID_VALUE;
+  }
+  return HCMIX_OK;
+}
+
+Rows flat(const void* p, size_t bytes) { return Rows{p, 1, bytes, bytes}; }
+
+Rows rows_of(const void* p, int64_t rows, int64_t stride, int64_t width, size_t elem) {
+  return Rows{p, (size_t)rows, (size_t)stride * elem, (size_t)width * elem};
+}
+
+constexpr int64_t kMaxStride = (int64_t)1 << 32;     // elements between two positions
+
+bool positive(float v) { return v > 0.f && v <= 3.4028235e38f; }
+
+// Head counts and strides of bf16 [..][heads][head_dim] operands.
+hcmix_status check_heads(int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
+  if (q_heads < 1 || kv_heads < 1 || head_dim < 1 || q_heads > 1024 || q_heads % kv_heads)
+    return HCMIX_ERR_INVALID_VALUE;
+  return head_dim == 64 || head_dim == 128 ? HCMIX_OK : HCMIX_ERR_UNSUPPORTED;
+}
+
+hcmix_status check_stride(int64_t stride, int64_t width) {
+  if (stride < width || stride > kMaxStride) return HCMIX_ERR_INVALID_VALUE;
+  return stride % 8 == 0 ? HCMIX_OK : HCMIX_ERR_UNSUPPORTED;
+}
+
+hcmix_status check_grouped(int64_t batch, int64_t n_q, int64_t n_k, int32_t q_heads,
+                           int32_t kv_heads, int32_t head_dim) {
+  if (batch < 1 || n_q < 1 || n_k < 1 || n_q > (1 << 20) || n_k > (1 << 20) ||
+      batch > kMaxRows / n_q || batch > kMaxRows / n_k)
+    return HCMIX_ERR_INVALID_VALUE;
+  return check_heads(q_heads, kv_heads, head_dim);
+}
+
+}  // namespace
+
+hcmix_status hcmix_rotary(int64_t rows, int32_t heads, int32_t head_dim, int32_t rot_dim,
+                          int32_t layout, int32_t inverse, int32_t dtype, const void* x,
+                          int64_t x_stride, const int32_t* positions, int64_t period,
+                          const double* freqs, float scale, void* y, int64_t y_stride,
+                          void* stream) {
+  if (!x || !freqs || !y) return HCMIX_ERR_INVALID_VALUE;
+  if (rows < 1 || rows > kMaxRows || heads < 1 || heads > 1024 || head_dim < 1 ||
+      head_dim > 512 || rot_dim < 1 || rot_dim > head_dim || (!positions && period < 1))
+    return HCMIX_ERR_INVALID_VALUE;
+  if (layout != HCMIX_ROTARY_HALF && layout != HCMIX_ROTARY_PAIRS) return HCMIX_ERR_INVALID_VALUE;
+  if (dtype != HCMIX_F32 && dtype != HCMIX_BF16) return HCMIX_ERR_INVALID_VALUE;
+  if (!(scale >= -3.4028235e38f && scale <= 3.4028235e38f)) return HCMIX_ERR_INVALID_VALUE;
+  const int64_t width = (int64_t)heads * head_dim;
+  if (x_stride < width || y_stride < width || x_stride > kMaxStride || y_stride > kMaxStride)
+    return HCMIX_ERR_INVALID_VALUE;
+  const size_t es = elem_size(dtype);
+  const Rows out = rows_of(y, rows, y_stride, width, es);
+  const Rows ins[3] = {flat(freqs, (size_t)rot_dim / 2 * sizeof(double)),
+                       flat(positions, positions ? (size_t)rows * sizeof(int32_t) : 0),
+                       rows_of(x, rows, x_stride, width, es)};
+  const bool in_place = x == y && x_stride == y_stride;
+  hcmix_status st = check_rows(ins, in_place ? 2 : 3, &out, 1);
+  if (st != HCMIX_OK) return st;
+  if (head_dim % 2 || rot_dim % 2 || !aligned(x, es) || !aligned(y, es) || !aligned(freqs, 8) ||
+      !aligned(positions, 4))
+    return HCMIX_ERR_UNSUPPORTED;
+  RotaryArgs a = {};
+  a.x = x;
+  a.y = y;
+  a.positions = positions;
+  a.freqs = freqs;
+  a.rows = rows;
+  a.x_stride = x_stride;
+  a.y_stride = y_stride;
+  a.period = period;
+  a.scale = scale;
+  a.heads = heads;
+  a.head_dim = head_dim;
+  a.rot = rot_dim;
+  a.inverse = inverse != 0;
+  hipError_t e = launch_rotary(a, layout == HCMIX_ROTARY_HALF, (int)es, (hipStream_t)stream);
+  return e == hipSuccess ? HCMIX_OK : hip_fail(e);
+}
+
+hcmix_status hcmix_grouped_attention_forward(
+    int64_t batch, int64_t n_q, int64_t n_k, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+    int32_t causal, float scale, const int32_t* lengths, const void* q, int64_t q_stride,
+    const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* out, float* lse,
+    void* stream) {
+  if (!q || !k || !v || !out || !lse) return HCMIX_ERR_INVALID_VALUE;
+  hcmix_status st = check_grouped(batch, n_q, n_k, q_heads, kv_heads, head_dim);
+  if (st != HCMIX_OK) return st;
+  if ((causal != 0 && causal != 1) || !positive(scale)) return HCMIX_ERR_INVALID_VALUE;
+  const int64_t qw = (int64_t)q_heads * head_dim, kw = (int64_t)kv_heads * head_dim;
+  if ((st = check_stride(q_stride, qw)) != HCMIX_OK || (st = check_stride(k_stride, kw)) != HCMIX_OK ||
+      (st = check_stride(v_stride, kw)) != HCMIX_OK)
+    return st;
+  const int64_t nq = batch * n_q, nk = batch * n_k;
+  const Rows ins[4] = {rows_of(q, nq, q_stride, qw, 2), rows_of(k, nk, k_stride, kw, 2),
+                       rows_of(v, nk, v_stride, kw, 2),
+                       flat(lengths, lengths ? (size_t)batch * sizeof(int32_t) : 0)};
+  const Rows outs[2] = {flat(out, (size_t)nq * qw * sizeof(bf16)),
+                        flat(lse, (size_t)nq * q_heads * sizeof(float))};
+  st = check_rows(ins, 4, outs, 2);
+  if (st != HCMIX_OK) return st;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) ||
+      !aligned(lse, 4) || !aligned(lengths, 4))
+    return HCMIX_ERR_UNSUPPORTED;
+  GroupedArgs a = {};
+  a.q = (const bf16*)q;
+  a.k = (const bf16*)k;
+  a.v = (const bf16*)v;
+  a.lengths = lengths;
+  a.out = (bf16*)out;
+  a.lse = lse;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.batch = (int)batch;
+  a.n_q = (int)n_q;
+  a.n_k = (int)n_k;
+  a.q_heads = q_heads;
+  a.kv_heads = kv_heads;
+  a.group = q_heads / kv_heads;
+  a.head_dim = head_dim;
+  a.causal = causal;
+  a.scale = scale;
+  hipError_t e = launch_grouped_forward(a, (hipStream_t)stream);
+  return e == hipSuccess ? HCMIX_OK : hip_fail(e);
+}
+
+size_t hcmix_grouped_attention_backward_workspace_bytes(int64_t batch, int64_t n_q, int64_t n_k,
+                                                        int32_t q_heads, int32_t kv_heads,
+                                                        int32_t head_dim) {
+  if (check_grouped(batch, n_q, n_k, q_heads, kv_heads, head_dim) != HCMIX_OK) return 0;
+  return grouped_workspace_bytes(batch, n_q, q_heads);
+}
+
+hcmix_status hcmix_grouped_attention_backward(
+    int64_t batch, int64_t n_q, int64_t n_k, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+    int32_t causal, float scale, const int32_t* lengths, const void* q, int64_t q_stride,
+    const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* out,
+    const float* lse, const void* dout, void* dq, int64_t dq_stride, void* dk, int64_t dk_stride,
+    void* dv, int64_t dv_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !k || !v || !out || !lse || !dout || !dq || !dk || !dv || !workspace)
+    return HCMIX_ERR_INVALID_VALUE;
+  hcmix_status st = check_grouped(batch, n_q, n_k, q_heads, kv_heads, head_dim);
+  if (st != HCMIX_OK) return st;
+  if ((causal != 0 && causal != 1) || !positive(scale)) return HCMIX_ERR_INVALID_VALUE;
+  const size_t need = grouped_workspace_bytes(batch, n_q, q_heads);
+  if (workspace_bytes < need) return HCMIX_ERR_INVALID_VALUE;
+  const int64_t qw = (int64_t)q_heads * head_dim, kw = (int64_t)kv_heads * head_dim;
+  const int64_t strides[6] = {q_stride, dq_stride, k_stride, v_stride, dk_stride, dv_stride};
+  for (int i = 0; i < 6; i++)
+    if ((st = check_stride(strides[i], i < 2 ? qw : kw)) != HCMIX_OK) return st;
+  const int64_t nq = batch * n_q, nk = batch * n_k;
+  const size_t act = (size_t)nq * qw * sizeof(bf16);
+  const Rows ins[7] = {rows_of(q, nq, q_stride, qw, 2), rows_of(k, nk, k_stride, kw, 2),
+                       rows_of(v, nk, v_stride, kw, 2), flat(out, act), flat(dout, act),
+                       flat(lse, (size_t)nq * q_heads * sizeof(float)),
+                       flat(lengths, lengths ? (size_t)batch * sizeof(int32_t) : 0)};
+  const Rows outs[4] = {rows_of(dq, nq, dq_stride, qw, 2), rows_of(dk, nk, dk_stride, kw, 2),
+                        rows_of(dv, nk, dv_stride, kw, 2), flat(workspace, need)};
+  st = check_rows(ins, 7, outs, 4);
+  if (st != HCMIX_OK) return st;
+  const void* wide[8] = {q, k, v, out, dout, dq, dk, dv};
+  for (const void* p : wide)
+    if (!aligned(p, 16)) return HCMIX_ERR_UNSUPPORTED;
+  if (!aligned(lse, 4) || !aligned(lengths, 4) || !aligned(workspace, 256))
+    return HCMIX_ERR_UNSUPPORTED;
+  GroupedArgs a = {};
+  a.q = (const bf16*)q;
+  a.k = (const bf16*)k;
+  a.v = (const bf16*)v;
+  a.lengths = lengths;
+  a.out = (bf16*)out;       // read
+  a.lse = (float*)lse;      // read
+  a.dout = (const bf16*)dout;
+  a.dq = (bf16*)dq;
+  a.dk = (bf16*)dk;
+  a.dv = (bf16*)dv;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.dq_stride = dq_stride;
+  a.dk_stride = dk_stride;
+  a.dv_stride = dv_stride;
+  a.batch = (int)batch;
+  a.n_q = (int)n_q;
+  a.n_k = (int)n_k;
+  a.q_heads = q_heads;
+  a.kv_heads = kv_heads;
+  a.group = q_heads / kv_heads;
+  a.head_dim = head_dim;
+  a.causal = causal;
+  a.scale = scale;
+  hipError_t e = launch_grouped_backward(a, workspace, (hipStream_t)stream);
+  return e == hipSuccess ? HCMIX_OK : hip_fail(e);
+}
+
+// ---- key/value cache in 8 bits ----
+
+namespace {
+
+hcmix_status check_kv(int64_t batch, int64_t capacity, int32_t kv_heads, int32_t head_dim) {
+  if (batch < 1 || batch > 65535 || capacity < 1 || capacity > (1 << 24) || kv_heads < 1 ||
+      kv_heads > 1024)
+    return HCMIX_ERR_INVALID_VALUE;
+  if (batch * kv_heads > kMaxElems / (2 * 128 * (capacity + kKvBlock)))
+    return HCMIX_ERR_INVALID_VALUE;
+  return check_heads(kv_heads, kv_heads, head_dim);
+}
+
+// Blocks of a sequence and head, and the cache's three parts.
+struct KvParts {
+  int blocks;
+  size_t values, scales, bytes;      // offsets of the parts, the whole
+};
+KvParts kv_parts(int64_t batch, int64_t capacity, int32_t kv_heads, int32_t head_dim) {
+  KvParts p;
+  p.blocks = (int)((capacity + kKvBlock - 1) / kKvBlock);
+  const size_t all = (size_t)batch * kv_heads * p.blocks;
+  p.values = all * kKvBlock * head_dim;
+  p.scales = 2 * p.values;
+  p.bytes = align256(p.scales + all * 2 * sizeof(float));
+  return p;
+}
+
+hcmix_status check_kv_call(int64_t batch, int64_t capacity, int32_t kv_heads, int32_t head_dim,
+                           int64_t tokens, const void* cache, size_t cache_bytes) {
+  hcmix_status st = check_kv(batch, capacity, kv_heads, head_dim);
+  if (st != HCMIX_OK) return st;
+  if (tokens < 1 || tokens > (1 << 16) || !cache) return HCMIX_ERR_INVALID_VALUE;
+  if (cache_bytes < kv_parts(batch, capacity, kv_heads, head_dim).bytes)
+    return HCMIX_ERR_INVALID_VALUE;
+  return aligned(cache, 256) ? HCMIX_OK : HCMIX_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+
+size_t hcmix_kv_cache_bytes(int64_t batch, int64_t capacity, int32_t kv_heads, int32_t head_dim) {
+  if (check_kv(batch, capacity, kv_heads, head_dim) != HCMIX_OK) return 0;
+  return kv_parts(batch, capacity, kv_heads, head_dim).bytes;
+}
+
+hcmix_status hcmix_kv_cache_append(int64_t batch, int64_t capacity, int32_t kv_heads,
+                                   int32_t head_dim, int64_t tokens, const void* k,
+                                   int64_t k_stride, const void* v, int64_t v_stride,
+                                   const int32_t* positions, const int32_t* counts, void* cache,
+                                   size_t cache_bytes, void* stream) {
+  if (!k || !v || !positions) return HCMIX_ERR_INVALID_VALUE;
+  hcmix_status st = check_kv_call(batch, capacity, kv_heads, head_dim, tokens, cache, cache_bytes);
+  if (st != HCMIX_OK) return st;
+  const int64_t kw = (int64_t)kv_heads * head_dim, rows = batch * tokens;
+  if ((st = check_stride(k_stride, kw)) != HCMIX_OK || (st = check_stride(v_stride, kw)) != HCMIX_OK)
+    return st;
+  const KvParts p = kv_parts(batch, capacity, kv_heads, head_dim);
+  const size_t ints = (size_t)batch * sizeof(int32_t);
+  const Rows ins[4] = {rows_of(k, rows, k_stride, kw, 2), rows_of(v, rows, v_stride, kw, 2),
+                       flat(positions, ints), flat(counts, counts ? ints : 0)};
+  const Rows out = flat(cache, p.bytes);
+  st = check_rows(ins, 4, &out, 1);
+  if (st != HCMIX_OK) return st;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(positions, 4) || !aligned(counts, 4))
+    return HCMIX_ERR_UNSUPPORTED;
+  KvAppendArgs a = {};
+  a.k = (const bf16*)k;
+  a.v = (const bf16*)v;
+  a.positions = positions;
+  a.counts = counts;
+  a.keys = (unsigned char*)cache;
+  a.values = a.keys + p.values;
+  a.scales = (float*)(a.keys + p.scales);
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.batch = (int)batch;
+  a.capacity = (int)capacity;
+  a.blocks = p.blocks;
+  a.tokens = (int)tokens;
+  a.kv_heads = kv_heads;
+  a.head_dim = head_dim;
+  hipError_t e = launch_kv_append(a, (hipStream_t)stream);
+  return e == hipSuccess ? HCMIX_OK : hip_fail(e);
+}
+
+hcmix_status hcmix_kv_cache_read(int64_t batch, int64_t capacity, int32_t kv_heads,
+                                 int32_t head_dim, int64_t tokens, const int32_t* first,
+                                 const int32_t* lengths, const void* cache, size_t cache_bytes,
+                                 void* k, void* v, void* stream) {
+  if (!first || !lengths || !k || !v) return HCMIX_ERR_INVALID_VALUE;
+  hcmix_status st = check_kv_call(batch, capacity, kv_heads, head_dim, tokens, cache, cache_bytes);
+  if (st != HCMIX_OK) return st;
+  const KvParts p = kv_parts(batch, capacity, kv_heads, head_dim);
+  const size_t ints = (size_t)batch * sizeof(int32_t);
+  const size_t act = (size_t)(batch * tokens) * kv_heads * head_dim * sizeof(bf16);
+  const Rows ins[3] = {flat(first, ints), flat(lengths, ints), flat(cache, p.bytes)};
+  const Rows outs[2] = {flat(k, act), flat(v, act)};
+  st = check_rows(ins, 3, outs, 2);
+  if (st != HCMIX_OK) return st;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(first, 4) || !aligned(lengths, 4))
+    return HCMIX_ERR_UNSUPPORTED;
+  KvReadArgs a = {};
+  a.keys = (const unsigned char*)cache;
+  a.values = a.keys + p.values;
+  a.scales = (const float*)(a.keys + p.scales);
+  a.first = first;
+  a.lengths = lengths;
+  a.k = (bf16*)k;
+  a.v = (bf16*)v;
+  a.batch = (int)batch;
+  a.capacity = (int)capacity;
+  a.blocks = p.blocks;
+  a.tokens = (int)tokens;
+  a.kv_heads = kv_heads;
+  a.head_dim = head_dim;
+  hipError_t e = launch_kv_read(a, (hipStream_t)stream);
+  return e == hipSuccess ? HCMIX_OK : hip_fail(e);
+}
+
+size_t hcmix_kv_cache_attention_workspace_bytes(int64_t batch, int64_t capacity, int32_t q_heads,
+                                                int32_t kv_heads, int32_t head_dim, int64_t tokens,
+                                                int64_t max_length) {
+  if (check_kv(batch, capacity, kv_heads, head_dim) != HCMIX_OK ||
+      check_heads(q_heads, kv_heads, head_dim) != HCMIX_OK || tokens < 1 || tokens > (1 << 16) ||
+      max_length < 1 || max_length > capacity)
+    return 0;
+  return kv_attention_workspace_bytes(batch, kv_heads, q_heads / kv_heads, head_dim, (int)tokens,
+                                      (int)max_length);
+}
+
+hcmix_status hcmix_kv_cache_attention(int64_t batch, int64_t capacity, int32_t q_heads,
+                                      int32_t kv_heads, int32_t head_dim, int64_t tokens,
+                                      float scale, const void* q, int64_t q_stride,
+                                      const int32_t* lengths, int64_t max_length,
+                                      const void* cache, size_t cache_bytes, void* out,
+                                      void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !lengths || !out) return HCMIX_ERR_INVALID_VALUE;
+  hcmix_status st = check_kv_call(batch, capacity, kv_heads, head_dim, tokens, cache, cache_bytes);
+  if (st != HCMIX_OK) return st;
+  if ((st = check_heads(q_heads, kv_heads, head_dim)) != HCMIX_OK) return st;
+  if (!positive(scale) || max_length < 1 || max_length > capacity) return HCMIX_ERR_INVALID_VALUE;
+  const int64_t qw = (int64_t)q_heads * head_dim, rows = batch * tokens;
+  if ((st = check_stride(q_stride, qw)) != HCMIX_OK) return st;
+  const KvParts p = kv_parts(batch, capacity, kv_heads, head_dim);
+  const size_t need = kv_attention_workspace_bytes(batch, kv_heads, q_heads / kv_heads, head_dim,
+                                                   (int)tokens, (int)max_length);
+  if (need && (!workspace || workspace_bytes < need)) return HCMIX_ERR_INVALID_VALUE;
+  const Rows ins[3] = {rows_of(q, rows, q_stride, qw, 2),
+                       flat(lengths, (size_t)batch * sizeof(int32_t)), flat(cache, p.bytes)};
+  const Rows outs[2] = {flat(out, (size_t)rows * qw * sizeof(bf16)), flat(workspace, need)};
+  st = check_rows(ins, 3, outs, need ? 2 : 1);
+  if (st != HCMIX_OK) return st;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lengths, 4) ||
+      (need && !aligned(workspace, 256)))
+    return HCMIX_ERR_UNSUPPORTED;
+  KvAttentionArgs a = {};
+  a.q = (const bf16*)q;
+  a.lengths = lengths;
+  a.keys = (const unsigned char*)cache;
+  a.values = a.keys + p.values;
+  a.scales = (const float*)(a.keys + p.scales);
+  a.out = (bf16*)out;
+  a.q_stride = q_stride;
+  a.batch = (int)batch;
+  a.capacity = (int)capacity;
+  a.blocks = p.blocks;
+  a.tokens = (int)tokens;
+  a.kv_heads = kv_heads;
+  a.group = q_heads / kv_heads;
+  a.head_dim = head_dim;
+  a.scale = scale;
+  hipError_t e = launch_kv_attention(a, workspace, (int)max_length, (hipStream_t)stream);
+  return e == hipSuccess ? HCMIX_OK : hip_fail(e);
+}

@@ -272,6 +272,77 @@ hipError_t launch_head_backward(const bf16* x, const bf16* w, const bf16* dl, bf
                                 int accumulate, float* workspace, size_t workspace_bytes, int rows,
                                 int width, int vocab, hipStream_t st);
 
+// ---- rotary positions ----
+struct RotaryArgs {
+  const void* x;
+  void* y;
+  const int* positions;        // null: row r stands at r % period
+  const double* freqs;         // radians per position, [rot / 2]
+  int64_t rows, x_stride, y_stride, period;
+  float scale;
+  int heads, head_dim, rot, inverse;
+  // set by launch_rotary: rows of a block, units of a head and 2^32 / units
+  // rounded up, log2 of the threads along a row
+  int rows_per_block, units, log_x;
+  uint64_t units_magic;
+};
+hipError_t launch_rotary(RotaryArgs a, int layout_half, int elem_bytes, hipStream_t st);
+
+// ---- attention over windows of any length, grouped heads ----
+// q, out, dout, dq: [batch][n_q][q_heads][head_dim]; k, v, dk, dv: [batch][n_k]
+// [kv_heads][head_dim]; positions `*_stride` elements apart (out and dout
+// contiguous); lse fp32 [batch][q_heads][n_q]; head_dim 64 or 128.
+struct GroupedArgs {
+  const bf16 *q, *k, *v;
+  const int* lengths;          // keys of each sequence, or null: n_k
+  bf16* out;
+  float* lse;
+  const bf16* dout;            // null in the forward, as all below
+  bf16 *dq, *dk, *dv;
+  float *row_sum, *row_lse;    // in the workspace
+  int64_t q_stride, k_stride, v_stride, dq_stride, dk_stride, dv_stride;
+  int batch, n_q, n_k, q_heads, kv_heads, group, head_dim, causal;
+  float scale;
+};
+size_t grouped_workspace_bytes(int64_t batch, int64_t n_q, int32_t q_heads);
+hipError_t launch_grouped_forward(const GroupedArgs& a, hipStream_t st);
+hipError_t launch_grouped_backward(GroupedArgs a, void* workspace, hipStream_t st);
+
+// ---- key/value cache in 8 bits ----
+constexpr int kKvBlock = 64;   // tokens that share a scale
+struct KvAppendArgs {
+  const bf16 *k, *v;           // [batch][tokens][kv_heads][head_dim], positions k_stride, v_stride apart
+  const int *positions, *counts;
+  unsigned char *keys, *values;
+  float* scales;
+  int64_t k_stride, v_stride;
+  int batch, capacity, blocks, tokens, kv_heads, head_dim;
+};
+struct KvReadArgs {
+  const unsigned char *keys, *values;
+  const float* scales;
+  const int *first, *lengths;
+  bf16 *k, *v;
+  int batch, capacity, blocks, tokens, kv_heads, head_dim;
+};
+struct KvAttentionArgs {
+  const bf16* q;
+  const int* lengths;
+  const unsigned char *keys, *values;
+  const float* scales;
+  bf16* out;
+  float *partial, *stats;      // in the workspace, when the sequences are split
+  int64_t q_stride;
+  int batch, capacity, blocks, tokens, kv_heads, group, head_dim, splits;
+  float scale;
+};
+hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st);
+hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t st);
+size_t kv_attention_workspace_bytes(int64_t batch, int32_t kv_heads, int32_t group,
+                                    int32_t head_dim, int32_t tokens, int32_t max_length);
+hipError_t launch_kv_attention(KvAttentionArgs a, void* workspace, int32_t max_length,
+                               hipStream_t st);
+
 struct DecodeLayerArgs {
   const bf16* x_in;
   const bf16* x_partner;

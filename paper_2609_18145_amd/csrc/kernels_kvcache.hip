@@ -1,0 +1,450 @@
+// Key/value cache in 8 bits and attention over it.
+//
+// A sequence's tokens lie in blocks of 64.  Every block of every key/value head
+// holds its keys and its values as e4m3 numbers (4 significant bits, largest
+// 448) times one power of two each, the least by which the largest value in the
+// block is at most 448.  A power of two costs no significant bit, and a block
+// whose scale has to grow for a later token is held again at the new one
+// without a second rounding (but of what then falls below 2^-6 of a unit, where
+// e4m3 has fewer bits).
+//
+// Layout, made for the attention's loads: for each (sequence, head, block)
+//   keys    [64 tokens][D] bytes
+//   values  [D][64] bytes, token t at kv_slot(t) of a row
+//   scales  fp32: keys, values
+// With the 16 x 16 x 32 matrix instruction S^T = K Q^T leaves lane (c = l % 16,
+// g = l / 16) with query c and keys 16 j + 4 g + 0..3 of each group j of 16, and
+// P V takes P from those registers when the values' fragment holds the same
+// keys: kv_slot puts a lane's 16 keys of the block in 16 consecutive bytes of
+// each dimension's row.  So both operands go from memory to registers to the
+// matrix instruction, with no LDS and no transposition, in 16-byte loads of
+// whole lines; the conversion to bf16 multiplies the scale in, exactly.
+#include "hcmix_internal.h"
+#include "device_common.h"
+
+namespace hcmix {
+
+namespace {
+
+constexpr int KV_THREADS = 256;
+constexpr int KV_WAVES = KV_THREADS / 64;
+constexpr int KB = kKvBlock;
+constexpr float KV_LOG2E = 1.4426950408889634f;
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ int kv_slot(int t) {
+  return 16 * ((t >> 2) & 3) + 8 * (t >> 5) + 4 * ((t >> 4) & 1) + (t & 3);
+}
+
+__device__ __forceinline__ int kv_bounded(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+// The least power of two, 2^-118 .. 2^120, by which amax divided is at most 448
+// = 1.75 2^8.
+__device__ __forceinline__ float kv_scale(float amax) {
+  const unsigned u = __float_as_uint(amax);
+  int e = (int)(u >> 23) - 127 - ((u & 0x7fffff) > 0x600000 ? 7 : 8);
+  e = kv_bounded(e, -118, 120);
+  return __uint_as_float((unsigned)(e + 127) << 23);
+}
+
+// |v| <= 448 (1 + 2^-9) or infinite: those are held as 448, NaN as NaN.
+__device__ __forceinline__ unsigned char kv_byte(float v) {
+  v = v > 448.f ? 448.f : v < -448.f ? -448.f : v;
+  return (unsigned char)__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false);
+}
+__device__ __forceinline__ float kv_value(unsigned byte) {
+  return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0);
+}
+
+// 16 bytes times `scale` (a power of two: exact) as two operand fragments.
+__device__ __forceinline__ void kv_expand(const u32x4& v, float scale, bf16x8* lo, bf16x8* hi) {
+#pragma unroll
+  for (int w = 0; w < 4; w++) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[w], scale, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[w], scale, true);
+    bf16x8& f = w < 2 ? *lo : *hi;
+    const int e = 4 * (w & 1);
+    f[e] = a[0];
+    f[e + 1] = a[1];
+    f[e + 2] = b[0];
+    f[e + 3] = b[1];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Append: a block of threads per touched block of one head and sequence.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(KV_THREADS) void kv_append_kernel(KvAppendArgs a) {
+  extern __shared__ unsigned char tile[];          // values of a fresh block: [D][64]
+  __shared__ float part[2][KV_WAVES];
+  const int h = blockIdx.y, b = blockIdx.z, D = a.head_dim;
+  const int pos = a.positions[b];
+  const int count = a.counts ? kv_bounded(a.counts[b], 0, a.tokens) : a.tokens;
+  if (pos < 0 || pos >= a.capacity) return;
+  const int end = a.capacity - pos < count ? a.capacity : pos + count;
+  const int blk = pos / KB + blockIdx.x, first = blk * KB;
+  const int t0 = first > pos ? first : pos, t1 = end < first + KB ? end : first + KB;
+  if (t0 >= t1) return;
+  const int old = t0 - first, n = t1 - t0;         // earlier tokens of the block, new ones
+  const size_t row0 = (size_t)b * a.tokens + (t0 - pos);
+  const bf16* k = a.k + row0 * a.k_stride + (size_t)h * D;
+  const bf16* v = a.v + row0 * a.v_stride + (size_t)h * D;
+  const size_t at = ((size_t)b * a.kv_heads + h) * a.blocks + blk;
+  unsigned char *ck = a.keys + at * KB * D, *cv = a.values + at * KB * D;
+  const int dv = D >> 3;                           // vectors of 8 of a row
+  float mk = 0.f, mv = 0.f;
+  for (int i = threadIdx.x; i < n * dv; i += KV_THREADS) {
+    const int t = i / dv, p = i - t * dv;
+    const bf16x8 x = *(const bf16x8*)(k + (size_t)t * a.k_stride + 8 * p);
+    const bf16x8 y = *(const bf16x8*)(v + (size_t)t * a.v_stride + 8 * p);
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      mk = fmaxf(mk, fabsf((float)x[e]));
+      mv = fmaxf(mv, fabsf((float)y[e]));
+    }
+  }
+#pragma unroll
+  for (int s = 32; s; s >>= 1) {
+    mk = fmaxf(mk, __shfl_xor(mk, s));
+    mv = fmaxf(mv, __shfl_xor(mv, s));
+  }
+  if ((threadIdx.x & 63) == 0) {
+    part[0][threadIdx.x >> 6] = mk;
+    part[1][threadIdx.x >> 6] = mv;
+  }
+  float *scales = a.scales + 2 * at;
+  const float ok = old ? scales[0] : 0.f, ov = old ? scales[1] : 0.f;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < KV_WAVES; w++) {
+    mk = fmaxf(mk, part[0][w]);
+    mv = fmaxf(mv, part[1][w]);
+  }
+  const float sk = fmaxf(kv_scale(mk), ok), sv = fmaxf(kv_scale(mv), ov);
+  if (threadIdx.x == 0) {
+    scales[0] = sk;
+    scales[1] = sv;
+  }
+  // what is there already, at the new scale
+  if (old && sk > ok)
+    for (int i = threadIdx.x; i < old * D; i += KV_THREADS) ck[i] = kv_byte(kv_value(ck[i]) * (ok / sk));
+  if (old && sv > ov)
+    for (int i = threadIdx.x; i < old * D; i += KV_THREADS) {
+      const int t = i % old, d = i / old;
+      unsigned char* c = cv + d * KB + kv_slot(t);
+      *c = kv_byte(kv_value(*c) * (ov / sv));
+    }
+  const float ik = 1.f / sk, iv = 1.f / sv;        // exact
+  if (!old)
+    for (int i = threadIdx.x; i < KB * D / 4; i += KV_THREADS) ((unsigned*)tile)[i] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n * dv; i += KV_THREADS) {
+    const int t = i / dv, p = i - t * dv;
+    const bf16x8 x = *(const bf16x8*)(k + (size_t)t * a.k_stride + 8 * p);
+    const bf16x8 y = *(const bf16x8*)(v + (size_t)t * a.v_stride + 8 * p);
+    unsigned w[2] = {0, 0};
+    unsigned char* out = old ? cv : tile;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      w[e >> 2] |= (unsigned)kv_byte((float)x[e] * ik) << (8 * (e & 3));
+      out[(8 * p + e) * KB + kv_slot(old + t)] = kv_byte((float)y[e] * iv);
+    }
+    *(uint2*)(ck + (size_t)(old + t) * D + 8 * p) = uint2{w[0], w[1]};
+  }
+  if (!old) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < KB * D / 16; i += KV_THREADS) ((u32x4*)cv)[i] = ((const u32x4*)tile)[i];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Read: tokens first[b] .. + tokens of every sequence, zeros from lengths[b] on.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(KV_THREADS) void kv_read_kernel(KvReadArgs a) {
+  const int h = blockIdx.y, b = blockIdx.z, D = a.head_dim, dv = D >> 3;
+  const int from = a.first[b], len = kv_bounded(a.lengths[b], 0, a.capacity);
+  const size_t at0 = ((size_t)b * a.kv_heads + h) * a.blocks;
+  for (int i = threadIdx.x; i < KB * dv; i += KV_THREADS) {
+    const int p = i / KB, t = blockIdx.x * KB + i % KB;    // neighbours read one dimension's row
+    if (t >= a.tokens) continue;
+    const int64_t pos = (int64_t)from + t;
+    bf16x8 x = {}, y = {};
+    if (pos >= 0 && pos < len) {
+      const size_t at = at0 + pos / KB;
+      const int r = (int)(pos % KB);
+      const float sk = a.scales[2 * at], sv = a.scales[2 * at + 1];
+      const uint2 w = *(const uint2*)(a.keys + at * KB * D + (size_t)r * D + 8 * p);
+      const unsigned char* c = a.values + at * KB * D + (size_t)8 * p * KB + kv_slot(r);
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        x[e] = to_bf16(kv_value(((e < 4 ? w.x : w.y) >> (8 * (e & 3))) & 255) * sk);
+        y[e] = to_bf16(kv_value(c[e * KB]) * sv);
+      }
+    }
+    const size_t o = (((size_t)b * a.tokens + t) * a.kv_heads + h) * D + 8 * p;
+    *(bf16x8*)(a.k + o) = x;
+    *(bf16x8*)(a.v + o) = y;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Attention: a block of four waves takes a range of the sequence's blocks for
+// one key/value head and 16 NQ of its query rows (token, head of the group);
+// its waves take the range's blocks in turn, each with its own running maximum
+// and sums, joined at the end.
+// ---------------------------------------------------------------------------
+template <int D, int NQ>
+__global__ __launch_bounds__(KV_THREADS) void kv_attention_kernel(KvAttentionArgs a) {
+  constexpr int KS = D / 32, DT = D / 16;
+  __shared__ float sm[KV_WAVES][16 * NQ], sl[KV_WAVES][16 * NQ];
+  __shared__ __attribute__((aligned(16))) float so[KV_WAVES][16][D + 4];
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int wave = wave_index<KV_WAVES>();
+  const int split = blockIdx.x % a.splits, rt = blockIdx.x / a.splits;
+  const int h = blockIdx.y, b = blockIdx.z;
+  const int rows = a.tokens * a.group, r0 = rt * 16 * NQ;
+  const int len = kv_bounded(__builtin_amdgcn_readfirstlane(a.lengths[b]), 0, a.capacity);
+  const int base = len - a.tokens;              // position of the first query token
+  // a row past the last repeats it and is not stored
+  bf16x8 q[NQ][KS];
+  int end[NQ];                                  // keys that this lane's row sees
+  int first_end = 1 << 30;                      // keys that all rows see
+#pragma unroll
+  for (int j = 0; j < NQ; j++) {
+    const int r = r0 + 16 * j + c < rows ? r0 + 16 * j + c : rows - 1;
+    const int t = r / a.group, qh = h * a.group + r - t * a.group;
+    const bf16* p = a.q + ((size_t)b * a.tokens + t) * a.q_stride + (size_t)qh * D;
+    end[j] = base + t + 1;
+#pragma unroll
+    for (int s = 0; s < KS; s++) q[j][s] = *(const bf16x8*)(p + (s >> 1) * 64 + 16 * g + 8 * (s & 1));
+  }
+  first_end = base + r0 / a.group + 1;
+  const int last_row = r0 + 16 * NQ < rows ? r0 + 16 * NQ - 1 : rows - 1;
+  const int last_end = base + last_row / a.group + 1;        // keys that any row sees, <= len
+  const int nblk = last_end > 0 ? (last_end + KB - 1) / KB : 0;
+  const int per = (nblk + a.splits - 1) / a.splits;
+  const int lo = split * per, hi = lo + per < nblk ? lo + per : nblk;
+  const size_t at0 = ((size_t)b * a.kv_heads + h) * a.blocks;
+  const float sc = a.scale * KV_LOG2E;
+  f32x4 o[NQ][DT] = {};
+  float m[NQ], l[NQ];
+#pragma unroll
+  for (int j = 0; j < NQ; j++) {
+    m[j] = -3e38f;
+    l[j] = 0.f;
+  }
+  for (int blk = lo + wave; blk < hi; blk += KV_WAVES) {
+    const size_t at = at0 + blk;
+    const unsigned char* ck = a.keys + at * KB * D;
+    const unsigned char* cv = a.values + at * KB * D;
+    u32x4 kr[4][D / 64], vr[DT];
+#pragma unroll
+    for (int t = 0; t < 4; t++)
+#pragma unroll
+      for (int s = 0; s < D / 64; s++)
+        kr[t][s] = *(const u32x4*)(ck + (16 * t + c) * D + 64 * s + 16 * g);
+#pragma unroll
+    for (int d = 0; d < DT; d++) vr[d] = *(const u32x4*)(cv + (16 * d + c) * KB + 16 * g);
+    const float2 scl = *(const float2*)(a.scales + 2 * at);
+    const int k0 = blk * KB;
+    if (k0 + KB > len) {
+      // the last block: values behind the last token may be anything, NaN among it
+      unsigned keep[4];
+#pragma unroll
+      for (int w = 0; w < 4; w++) {
+        // byte 4 w + r of a lane: key 32 (w / 2) + 16 (w % 2) + 4 g + r
+        const int left = len - (k0 + 32 * (w >> 1) + 16 * (w & 1) + 4 * g);
+        keep[w] = left >= 4 ? ~0u : left <= 0 ? 0u : ~0u >> (32 - 8 * left);
+      }
+#pragma unroll
+      for (int d = 0; d < DT; d++)
+#pragma unroll
+        for (int w = 0; w < 4; w++) vr[d][w] &= keep[w];
+    }
+    f32x4 s[NQ][4];
+#pragma unroll
+    for (int t = 0; t < 4; t++) {
+      bf16x8 kf[KS];
+#pragma unroll
+      for (int u = 0; u < D / 64; u++) kv_expand(kr[t][u], scl.x, &kf[2 * u], &kf[2 * u + 1]);
+#pragma unroll
+      for (int j = 0; j < NQ; j++) {
+        s[j][t] = f32x4{};
+#pragma unroll
+        for (int u = 0; u < KS; u++) s[j][t] = mfma16(kf[u], q[j][u], s[j][t]);
+      }
+    }
+    if (k0 + KB > first_end) {
+#pragma unroll
+      for (int j = 0; j < NQ; j++)
+#pragma unroll
+        for (int t = 0; t < 4; t++)
+#pragma unroll
+          for (int r = 0; r < 4; r++)
+            if (k0 + 16 * t + 4 * g + r >= end[j]) s[j][t][r] = -INFINITY;
+    }
+    bf16x8 p[NQ][2];
+#pragma unroll
+    for (int j = 0; j < NQ; j++) {
+      float mx = s[j][0][0];
+#pragma unroll
+      for (int t = 0; t < 4; t++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) mx = fmaxf(mx, s[j][t][r]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32)) * sc;
+      const float mn = fmaxf(m[j], mx), alpha = __builtin_amdgcn_exp2f(m[j] - mn);
+      m[j] = mn;
+      l[j] *= alpha;
+#pragma unroll
+      for (int d = 0; d < DT; d++) o[j][d] *= alpha;
+#pragma unroll
+      for (int t = 0; t < 4; t++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(s[j][t][r], sc, -mn));
+          l[j] += e;
+          p[j][t >> 1][4 * (t & 1) + r] = to_bf16(e);
+        }
+    }
+#pragma unroll
+    for (int d = 0; d < DT; d++) {
+      bf16x8 lo8, hi8;
+      kv_expand(vr[d], scl.y, &lo8, &hi8);
+#pragma unroll
+      for (int j = 0; j < NQ; j++) {
+        o[j][d] = mfma16(lo8, p[j][0], o[j][d]);
+        o[j][d] = mfma16(hi8, p[j][1], o[j][d]);
+      }
+    }
+  }
+  // join the waves: o[j][d] register r of a lane: row 16 j + c, dimension 16 d + 4 g + r
+#pragma unroll
+  for (int j = 0; j < NQ; j++) {
+    l[j] += __shfl_xor(l[j], 16);
+    l[j] += __shfl_xor(l[j], 32);
+    if (g == 0) {
+      sm[wave][16 * j + c] = m[j];
+      sl[wave][16 * j + c] = l[j];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NQ; j++) {
+    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < DT; d++) *(f32x4*)&so[wave][c][16 * d + 4 * g] = o[j][d];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * D / 4; i += KV_THREADS) {
+      const int row = i / (D / 4), d4 = i % (D / 4), r = r0 + 16 * j + row;
+      if (r >= rows) continue;
+      float mm = -3e38f, ll = 0.f;
+#pragma unroll
+      for (int w = 0; w < KV_WAVES; w++) mm = fmaxf(mm, sm[w][16 * j + row]);
+      f32x4 acc = {};
+#pragma unroll
+      for (int w = 0; w < KV_WAVES; w++) {
+        const float f = __builtin_amdgcn_exp2f(sm[w][16 * j + row] - mm);
+        ll += f * sl[w][16 * j + row];
+        acc += f * *(const f32x4*)&so[w][row][4 * d4];
+      }
+      const size_t part = (((size_t)b * a.kv_heads + h) * rows + r) * a.splits + split;
+      if (a.splits > 1) {
+        *(f32x4*)(a.partial + part * D + 4 * d4) = acc;
+        if (d4 == 0) *(float2*)(a.stats + 2 * part) = float2{mm, ll};
+      } else {
+        const int t = r / a.group, qh = h * a.group + r - t * a.group;
+        const float inv = ll == 0.f ? 0.f : 1.f / ll;       // 0: the row sees nothing
+        bf16x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; e++) y[e] = to_bf16(acc[e] * inv);
+        *(bf16x4*)(a.out + (((size_t)b * a.tokens + t) * a.kv_heads * a.group + qh) * D + 4 * d4) = y;
+      }
+    }
+  }
+}
+
+// Joins the ranges of a row: D / 4 threads per row.
+__global__ __launch_bounds__(KV_THREADS) void kv_join_kernel(KvAttentionArgs a, int D, int64_t total) {
+  const int64_t i = (int64_t)blockIdx.x * KV_THREADS + threadIdx.x;
+  const int64_t row = i / (D / 4);
+  const int d4 = (int)(i - row * (D / 4));
+  if (row >= total) return;
+  float mm = -3e38f, ll = 0.f;
+  for (int s = 0; s < a.splits; s++) mm = fmaxf(mm, a.stats[2 * (row * a.splits + s)]);
+  f32x4 acc = {};
+  for (int s = 0; s < a.splits; s++) {
+    const size_t p = row * a.splits + s;
+    const float2 st = *(const float2*)(a.stats + 2 * p);
+    const float f = __builtin_amdgcn_exp2f(st.x - mm);
+    ll += f * st.y;
+    acc += f * *(const f32x4*)(a.partial + p * D + 4 * d4);
+  }
+  const int rows = a.tokens * a.group;
+  const int64_t bh = row / rows, b = bh / a.kv_heads;
+  const int r = (int)(row - bh * rows), h = (int)(bh - b * a.kv_heads);
+  const int t = r / a.group, qh = h * a.group + r - t * a.group;
+  const float inv = ll == 0.f ? 0.f : 1.f / ll;
+  bf16x4 y;
+#pragma unroll
+  for (int e = 0; e < 4; e++) y[e] = to_bf16(acc[e] * inv);
+  *(bf16x4*)(a.out + (((size_t)b * a.tokens + t) * a.kv_heads * a.group + qh) * D + 4 * d4) = y;
+}
+
+int kv_row_tiles(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }     // NQ
+
+// Ranges of a sequence: enough blocks of threads for the chip (two to a CU),
+// each with at least two of the sequence's blocks for every wave.
+int kv_splits(int64_t batch, int kv_heads, int rows, int max_length) {
+  const int nq = kv_row_tiles(rows);
+  const int64_t blocks = batch * kv_heads * ((rows + 16 * nq - 1) / (16 * nq));
+  const int64_t want = (512 + blocks - 1) / blocks;
+  const int64_t most = ((max_length + KB - 1) / KB + 2 * KV_WAVES - 1) / (2 * KV_WAVES);
+  const int64_t s = want < most ? want : most;
+  return s < 1 ? 1 : (int)s;
+}
+
+template <int D>
+hipError_t kv_attention_launch(const KvAttentionArgs& a, hipStream_t st) {
+  const int rows = a.tokens * a.group, nq = kv_row_tiles(rows);
+  const dim3 grid(a.splits * ((rows + 16 * nq - 1) / (16 * nq)), a.kv_heads, a.batch);
+  if (nq == 1) kv_attention_kernel<D, 1><<<grid, KV_THREADS, 0, st>>>(a);
+  else if (nq == 2) kv_attention_kernel<D, 2><<<grid, KV_THREADS, 0, st>>>(a);
+  else kv_attention_kernel<D, 4><<<grid, KV_THREADS, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t total = (int64_t)a.batch * a.kv_heads * rows;
+  kv_join_kernel<<<(int)((total * (D / 4) + KV_THREADS - 1) / KV_THREADS), KV_THREADS, 0, st>>>(a, D, total);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st) {
+  const dim3 grid((a.tokens + KB - 2) / KB + 1, a.kv_heads, a.batch);
+  kv_append_kernel<<<grid, KV_THREADS, KB * a.head_dim, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t st) {
+  const dim3 grid((a.tokens + KB - 1) / KB, a.kv_heads, a.batch);
+  kv_read_kernel<<<grid, KV_THREADS, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+size_t kv_attention_workspace_bytes(int64_t batch, int32_t kv_heads, int32_t group,
+                                    int32_t head_dim, int32_t tokens, int32_t max_length) {
+  const int splits = kv_splits(batch, kv_heads, tokens * group, max_length);
+  if (splits == 1) return 0;
+  const size_t parts = (size_t)batch * kv_heads * tokens * group * splits;
+  return parts * (head_dim + 2) * sizeof(float) / 256 * 256 + 256;
+}
+
+hipError_t launch_kv_attention(KvAttentionArgs a, void* workspace, int32_t max_length,
+                               hipStream_t st) {
+  a.splits = kv_splits(a.batch, a.kv_heads, a.tokens * a.group, max_length);
+  a.partial = (float*)workspace;
+  a.stats = a.partial + (size_t)a.batch * a.kv_heads * a.tokens * a.group * a.splits * a.head_dim;
+  return a.head_dim == 64 ? kv_attention_launch<64>(a, st) : kv_attention_launch<128>(a, st);
+}
+
+}  // namespace hcmix

@@ -11,6 +11,15 @@ the first call with GPU tensors: there is no CPU or PyTorch fallback.
     y = Stack.apply(x, layers, causal, *w_selfs, *w_offs)   # autograd over L layers
     y, m, lse, partners = field_forward(p, x, tau, scaled, workspace=ws)
     dp, dx = field_backward(p, x, m, lse, dy, tau, scaled, workspace=ws, reuse_table=True)
+
+Attention layers of any length (q [batch, n, heads, head_dim], k and v with fewer
+heads, slices of a packed projection among them), and their decoding:
+
+    q = rotary(q, freqs)
+    out, lse = grouped_attention_forward(q, k, v, causal, lengths)
+    dq, dk, dv = grouped_attention_backward(q, k, v, out, lse, dout, causal, lengths)
+    kv_cache_append(k, v, positions, cache, capacity)
+    out = kv_cache_attention(q, lengths, cache, capacity, kv_heads)
 """
 from __future__ import annotations
 
@@ -18,6 +27,7 @@ import array
 import ctypes
 import importlib.machinery
 import importlib.util
+import math
 import os
 
 import torch
@@ -46,7 +56,11 @@ EXPORTS = ("hcmix_status_string", "hcmix_last_hip_error", "hcmix_dim", "hcmix_fo
            "hcmix_shared_stack_backward_workspace_bytes", "hcmix_shared_stack_backward",
            "hcmix_linear_forward", "hcmix_linear_backward_workspace_bytes",
            "hcmix_linear_backward", "hcmix_field_forward", "hcmix_field_workspace_bytes",
-           "hcmix_field_backward")
+           "hcmix_field_backward", "hcmix_rotary", "hcmix_grouped_attention_forward",
+           "hcmix_grouped_attention_backward_workspace_bytes",
+           "hcmix_grouped_attention_backward", "hcmix_kv_cache_bytes", "hcmix_kv_cache_append",
+           "hcmix_kv_cache_read", "hcmix_kv_cache_attention_workspace_bytes",
+           "hcmix_kv_cache_attention")
 
 _lib = None
 _marshal = None
@@ -149,6 +163,31 @@ def load():
         lib.hcmix_linear_backward_workspace_bytes.restype = sz
         lib.hcmix_linear_backward.argtypes = [i64, i64, i64, vp, vp, vp, vp, fp, i32, vp, sz, vp]
         lib.hcmix_linear_backward.restype = i32
+        f32 = ctypes.c_float
+        lib.hcmix_rotary.argtypes = [i64, i32, i32, i32, i32, i32, i32, vp, i64, ip, i64, vp, f32,
+                                     vp, i64, vp]
+        lib.hcmix_rotary.restype = i32
+        grouped = [i64, i64, i64, i32, i32, i32, i32, f32, ip, vp, i64, vp, i64, vp, i64, vp, fp]
+        lib.hcmix_grouped_attention_forward.argtypes = [*grouped, vp]
+        lib.hcmix_grouped_attention_forward.restype = i32
+        lib.hcmix_grouped_attention_backward_workspace_bytes.argtypes = [i64, i64, i64, i32, i32,
+                                                                         i32]
+        lib.hcmix_grouped_attention_backward_workspace_bytes.restype = sz
+        lib.hcmix_grouped_attention_backward.argtypes = [*grouped, vp, vp, i64, vp, i64, vp, i64,
+                                                         vp, sz, vp]
+        lib.hcmix_grouped_attention_backward.restype = i32
+        lib.hcmix_kv_cache_bytes.argtypes = [i64, i64, i32, i32]
+        lib.hcmix_kv_cache_bytes.restype = sz
+        lib.hcmix_kv_cache_append.argtypes = [i64, i64, i32, i32, i64, vp, i64, vp, i64, ip, ip,
+                                              vp, sz, vp]
+        lib.hcmix_kv_cache_append.restype = i32
+        lib.hcmix_kv_cache_read.argtypes = [i64, i64, i32, i32, i64, ip, ip, vp, sz, vp, vp, vp]
+        lib.hcmix_kv_cache_read.restype = i32
+        lib.hcmix_kv_cache_attention_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i64, i64]
+        lib.hcmix_kv_cache_attention_workspace_bytes.restype = sz
+        lib.hcmix_kv_cache_attention.argtypes = [i64, i64, i32, i32, i32, i64, f32, vp, i64, ip,
+                                                 i64, vp, sz, vp, vp, sz, vp]
+        lib.hcmix_kv_cache_attention.restype = i32
         _lib = lib
     return _lib
 
@@ -908,6 +947,306 @@ def linear_backward(x, w, dy, dx=None, dw=None, with_dx=True, with_dw=True, accu
     if rc != HCMIX_OK:
         raise HcmixError(rc, "hcmix_linear_backward")
     return (dx if want_dx else None), (dw if want_dw else None)
+
+
+# ---- attention layers past the fixed windows ----
+
+_ROTARY_LAYOUTS = {"half": 0, "pairs": 1}
+
+
+def _call(dev, what, *args):
+    """A library call on dev's current stream, with dev the current device (a
+    kernel is launched on the current device's behalf)."""
+    fn = getattr(load(), what)
+    if dev.index == torch.cuda.current_device():
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+    if rc != HCMIX_OK:
+        raise HcmixError(rc, what)
+
+
+def _heads(t, name, shape, dtype, device=None):
+    """Checks a [batch, n, heads, head_dim] operand (None entries match any
+    extent): heads side by side, positions evenly spaced over the whole batch, as
+    in a slice of a packed projection.  Returns the elements between positions."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name}: expected a tensor, got {type(t).__name__}")
+    got = tuple(t.shape)
+    if len(got) != 4 or any(e is not None and g != e for g, e in zip(got, shape)):
+        raise ValueError(f"{name}: shape {got}, expected {tuple(shape)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: on {t.device}, expected {device}")
+    b, n, h, d = got
+    sb, sn, sh, sd = t.stride()
+    stride = sn if n > 1 else sb if b > 1 else h * d
+    if ((d > 1 and sd != 1) or (h > 1 and sh != d) or (n > 1 and b > 1 and sb != n * sn)
+            or stride < h * d):
+        raise ValueError(f"{name}: strides {t.stride()}, expected positions evenly spaced over the "
+                         "batch, their heads contiguous")
+    return stride
+
+
+def rotary_frequencies(rot_dim, base=10000.0, scaling=None, factor=1.0, original_length=None,
+                       turns=(1.0, 32.0), device="cuda"):
+    """(freqs, scale) for ``rotary``: fp64 [rot_dim / 2] radians per position,
+    freqs[j] = base^(-2j / rot_dim), and the factor on the turned values (1 but for
+    "yarn").  scaling, for contexts `factor` times the original one:
+      "linear"  every frequency divided by factor;
+      "ntk"     base times factor^(rot_dim / (rot_dim - 2)): the slowest pair is
+                divided by factor, the fastest stays;
+      "yarn"    pairs that turn more than turns[1] times within original_length stay,
+                those that turn less than turns[0] times are divided by factor, in
+                between linearly in the number of turns; scale 0.1 ln(factor) + 1."""
+    if rot_dim < 2 or rot_dim % 2:
+        raise ValueError(f"rot_dim: {rot_dim}, expected an even number of at least 2")
+    if not base > 0 or not factor >= 1:
+        raise ValueError(f"base {base}, factor {factor}: expected base > 0, factor >= 1")
+    if scaling not in (None, "linear", "ntk", "yarn"):
+        raise ValueError(f"scaling: {scaling!r}, expected None, 'linear', 'ntk' or 'yarn'")
+    scale = 1.0
+    if scaling == "ntk" and rot_dim > 2:
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    j = torch.arange(0, rot_dim, 2, dtype=torch.float64)
+    freqs = base ** (-j / rot_dim)
+    if scaling == "linear":
+        freqs = freqs / factor
+    elif scaling == "yarn":
+        if original_length is None or original_length < 1 or not turns[0] < turns[1]:
+            raise ValueError("yarn: expected original_length >= 1 and turns[0] < turns[1]")
+        t = original_length * freqs / (2 * math.pi)
+        keep = ((t - turns[0]) / (turns[1] - turns[0])).clamp(0, 1)
+        freqs = keep * freqs + (1 - keep) * (freqs / factor)
+        scale = 0.1 * math.log(factor) + 1.0
+    return freqs.to(device), scale
+
+
+def rotary(x, freqs, positions=None, layout="half", inverse=False, scale=1.0, out=None):
+    """x [batch, n, heads, head_dim] (bf16 or fp32; positions may be spaced, as in
+    a slice of a packed projection) with the first 2 len(freqs) values of every
+    head turned by position * freqs.  positions: int32 [batch, n], default 0 .. n - 1
+    in every sequence.  layout: pairs (j, j + rot / 2) ("half") or (2j, 2j + 1)
+    ("pairs").  inverse: by the opposite angle, the backward.  out: x itself (in
+    place), or a tensor that shares nothing with it."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 4:
+        raise ValueError("x: expected a [batch, n, heads, head_dim] tensor")
+    if layout not in _ROTARY_LAYOUTS:
+        raise ValueError(f"layout: {layout!r}, expected 'half' or 'pairs'")
+    dt = _act_dtype(x)
+    x_stride = _heads(x, "x", (None,) * 4, dt)
+    dev = x.device
+    batch, n, heads, hd = x.shape
+    _need(freqs, "freqs", (None,), torch.float64, dev)
+    if positions is not None:
+        _need(positions, "positions", (batch, n), torch.int32, dev)
+    if out is None:
+        out = torch.empty((batch, n, heads, hd), dtype=dt, device=dev)
+    y_stride = _heads(out, "out", tuple(x.shape), dt, dev)
+    _gpu(dev)
+    _call(dev, "hcmix_rotary", batch * n, heads, hd, 2 * freqs.numel(), _ROTARY_LAYOUTS[layout],
+          int(bool(inverse)), _dtype_code(x), _ptr(x), x_stride, _ptr(positions), n, _ptr(freqs),
+          float(scale), _ptr(out), y_stride)
+    return out
+
+
+def _grouped_operands(q, k, v, lengths):
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q: expected a [batch, n, heads, head_dim] tensor")
+    bf = torch.bfloat16
+    batch, n_q, q_heads, hd = q.shape
+    qs = _heads(q, "q", (None,) * 4, bf)
+    dev = q.device
+    ks = _heads(k, "k", (batch, None, None, hd), bf, dev)
+    n_k, kv_heads = k.shape[1:3]
+    vs = _heads(v, "v", (batch, n_k, kv_heads, hd), bf, dev)
+    if lengths is not None:
+        _need(lengths, "lengths", (batch,), torch.int32, dev)
+    return dev, (batch, n_q, n_k, q_heads, kv_heads, hd), (qs, ks, vs)
+
+
+def grouped_attention_forward(q, k, v, causal=True, lengths=None, scale=None, out=None, lse=None):
+    """Attention over sequences of any length: q [batch, n_q, q_heads, hd], k and v
+    [batch, n_k, kv_heads, hd] bf16, hd 64 or 128 (slices of a packed projection
+    as they are); query head h takes key/value head h // (q_heads // kv_heads).
+    lengths: int32 [batch], the keys of each sequence that count; causal: query i
+    sees keys up to i + n_k - n_q.  scale defaults to hd ** -0.5.  Returns (out
+    bf16 like q, contiguous; lse fp32 [batch, q_heads, n_q]); a row that sees
+    nothing gives 0 and -inf."""
+    dev, dims, (qs, ks, vs) = _grouped_operands(q, k, v, lengths)
+    batch, n_q, _, q_heads, _, hd = dims
+    if out is None:
+        out = torch.empty((batch, n_q, q_heads, hd), dtype=q.dtype, device=dev)
+    if lse is None:
+        lse = torch.empty((batch, q_heads, n_q), dtype=torch.float32, device=dev)
+    _need(out, "out", (batch, n_q, q_heads, hd), torch.bfloat16, dev)
+    _need(lse, "lse", (batch, q_heads, n_q), torch.float32, dev)
+    _gpu(dev)
+    _call(dev, "hcmix_grouped_attention_forward", *dims, int(bool(causal)),
+          hd ** -0.5 if scale is None else float(scale), _ptr(lengths), _ptr(q), qs, _ptr(k), ks,
+          _ptr(v), vs, _ptr(out), _ptr(lse))
+    return out, lse
+
+
+def grouped_attention_backward(q, k, v, out, lse, dout, causal=True, lengths=None, scale=None,
+                               dq=None, dk=None, dv=None, workspace=None):
+    """(dq, dk, dv) of ``grouped_attention_forward`` given its results and dout =
+    dL/dout (contiguous).  dq, dk, dv may be slices of one packed buffer."""
+    dev, dims, (qs, ks, vs) = _grouped_operands(q, k, v, lengths)
+    batch, n_q, n_k, q_heads, kv_heads, hd = dims
+    bf = torch.bfloat16
+    _need(out, "out", (batch, n_q, q_heads, hd), bf, dev)
+    _need(lse, "lse", (batch, q_heads, n_q), torch.float32, dev)
+    _need(dout, "dout", (batch, n_q, q_heads, hd), bf, dev)
+    dq, dk, dv = (torch.empty(t.shape, dtype=bf, device=dev) if g is None else g
+                  for g, t in ((dq, q), (dk, k), (dv, v)))
+    dqs = _heads(dq, "dq", tuple(q.shape), bf, dev)
+    dks = _heads(dk, "dk", tuple(k.shape), bf, dev)
+    dvs = _heads(dv, "dv", tuple(v.shape), bf, dev)
+    _gpu(dev)
+    if workspace is None:
+        nbytes = load().hcmix_grouped_attention_backward_workspace_bytes(*dims)
+        workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=dev)
+    _call(dev, "hcmix_grouped_attention_backward", *dims, int(bool(causal)),
+          hd ** -0.5 if scale is None else float(scale), _ptr(lengths), _ptr(q), qs, _ptr(k), ks,
+          _ptr(v), vs, _ptr(out), _ptr(lse), _ptr(dout), _ptr(dq), dqs, _ptr(dk), dks, _ptr(dv),
+          dvs, _ptr(workspace), _workspace_bytes(workspace, dev))
+    return dq, dk, dv
+
+
+def _workspace_bytes(t, dev):
+    if t is not None and isinstance(t, torch.Tensor) and t.device != dev:
+        raise ValueError(f"workspace/cache: on {t.device}, expected {dev}")
+    return _bytes(t)
+
+
+def kv_cache_bytes(batch, capacity, kv_heads, head_dim) -> int:
+    return load().hcmix_kv_cache_bytes(batch, capacity, kv_heads, head_dim)
+
+
+def alloc_kv_cache(batch, capacity, kv_heads, head_dim, device):
+    """Device memory for `capacity` tokens of every sequence, keys and values in 8
+    bits with a scale for each block of 64 tokens and head (no initialisation)."""
+    nbytes = kv_cache_bytes(batch, capacity, kv_heads, head_dim)
+    if nbytes == 0:
+        raise ValueError(f"kv cache: batch {batch}, capacity {capacity}, kv_heads {kv_heads}, "
+                         f"head_dim {head_dim} is not supported")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _cache(cache, dev):
+    if not isinstance(cache, torch.Tensor) or cache.device != dev:
+        raise ValueError(f"cache: expected a tensor on {dev}")
+
+
+def kv_cache_append(k, v, positions, cache, capacity, counts=None):
+    """Puts k, v [batch, tokens, kv_heads, hd] bf16 (positions may be spaced) at
+    positions[b] and behind (int32 [batch] on the GPU), the first counts[b] of every
+    sequence where counts is given.  What was held from positions[b] on is
+    dropped; tokens at `capacity` and behind are left out."""
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+        raise ValueError("k: expected a [batch, tokens, kv_heads, head_dim] tensor")
+    ks = _heads(k, "k", (None,) * 4, torch.bfloat16)
+    dev = k.device
+    batch, tokens, kv_heads, hd = k.shape
+    vs = _heads(v, "v", tuple(k.shape), torch.bfloat16, dev)
+    _need(positions, "positions", (batch,), torch.int32, dev)
+    if counts is not None:
+        _need(counts, "counts", (batch,), torch.int32, dev)
+    _cache(cache, dev)
+    _gpu(dev)
+    _call(dev, "hcmix_kv_cache_append", batch, capacity, kv_heads, hd, tokens, _ptr(k), ks,
+          _ptr(v), vs, _ptr(positions), _ptr(counts), _ptr(cache), _bytes(cache))
+    return cache
+
+
+def kv_cache_read(cache, capacity, kv_heads, head_dim, first, lengths, tokens, k=None, v=None):
+    """(k, v) bf16 [batch, tokens, kv_heads, head_dim]: the values held for tokens
+    first[b] and behind, 0 outside 0 .. lengths[b] - 1 (int32 [batch] on the GPU)."""
+    if not isinstance(first, torch.Tensor) or first.dim() != 1:
+        raise ValueError("first: expected a [batch] tensor")
+    batch, dev = first.shape[0], first.device
+    _need(first, "first", None, torch.int32)
+    _need(lengths, "lengths", (batch,), torch.int32, dev)
+    _cache(cache, dev)
+    shape = (batch, tokens, kv_heads, head_dim)
+    k, v = (torch.empty(shape, dtype=torch.bfloat16, device=dev) if t is None else t
+            for t in (k, v))
+    _need(k, "k", shape, torch.bfloat16, dev)
+    _need(v, "v", shape, torch.bfloat16, dev)
+    _gpu(dev)
+    _call(dev, "hcmix_kv_cache_read", batch, capacity, kv_heads, head_dim, tokens, _ptr(first),
+          _ptr(lengths), _ptr(cache), _bytes(cache), _ptr(k), _ptr(v))
+    return k, v
+
+
+def kv_cache_attention(q, lengths, cache, capacity, kv_heads, scale=None, max_length=None,
+                       out=None, workspace=None):
+    """Attention of q [batch, tokens, q_heads, hd] bf16 over the cache, the last
+    token standing at lengths[b] - 1 (int32 [batch] on the GPU, the new tokens
+    included): every token sees those up to itself.  scale defaults to hd ** -0.5;
+    max_length: how long sequences are expected to be (default: capacity)."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q: expected a [batch, tokens, q_heads, head_dim] tensor")
+    qs = _heads(q, "q", (None,) * 4, torch.bfloat16)
+    dev = q.device
+    batch, tokens, q_heads, hd = q.shape
+    _need(lengths, "lengths", (batch,), torch.int32, dev)
+    _cache(cache, dev)
+    if out is None:
+        out = torch.empty((batch, tokens, q_heads, hd), dtype=torch.bfloat16, device=dev)
+    _need(out, "out", (batch, tokens, q_heads, hd), torch.bfloat16, dev)
+    _gpu(dev)
+    longest = capacity if max_length is None else max_length
+    if workspace is None:
+        nbytes = load().hcmix_kv_cache_attention_workspace_bytes(batch, capacity, q_heads, kv_heads,
+                                                                 hd, tokens, longest)
+        if nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _call(dev, "hcmix_kv_cache_attention", batch, capacity, q_heads, kv_heads, hd, tokens,
+          hd ** -0.5 if scale is None else float(scale), _ptr(q), qs, _ptr(lengths), longest,
+          _ptr(cache), _bytes(cache), _ptr(out), _ptr(workspace), _workspace_bytes(workspace, dev))
+    return out
+
+
+class Rotary(torch.autograd.Function):
+    """``rotary`` as an autograd function over x.
+
+    Rotary.apply(x, freqs, positions, layout, scale) -> y"""
+
+    @staticmethod
+    def forward(ctx, x, freqs, positions=None, layout="half", scale=1.0):
+        ctx.layout, ctx.scale = layout, scale
+        ctx.save_for_backward(freqs, positions)
+        return rotary(x, freqs, positions, layout, False, scale)
+
+    @staticmethod
+    def backward(ctx, gy):
+        freqs, positions = ctx.saved_tensors
+        return (rotary(gy.contiguous(), freqs, positions, ctx.layout, True, ctx.scale), None, None,
+                None, None)
+
+
+class GroupedAttention(torch.autograd.Function):
+    """Attention over sequences of any length as an autograd function over q, k, v.
+
+    GroupedAttention.apply(q, k, v, causal, lengths, scale) -> out"""
+
+    @staticmethod
+    def forward(ctx, q, k, v, causal=True, lengths=None, scale=None):
+        out, lse = grouped_attention_forward(q, k, v, causal, lengths, scale)
+        ctx.causal, ctx.scale = causal, scale
+        ctx.save_for_backward(q, k, v, out, lse, lengths)
+        return out
+
+    @staticmethod
+    def backward(ctx, gout):
+        q, k, v, out, lse, lengths = ctx.saved_tensors
+        dq, dk, dv = grouped_attention_backward(q, k, v, out, lse, gout.contiguous(), ctx.causal,
+                                                lengths, ctx.scale)
+        return dq, dk, dv, None, None, None
 
 
 class Attention(torch.autograd.Function):

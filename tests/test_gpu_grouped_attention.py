@@ -1,0 +1,176 @@
+"""Attention over windows of any length against the oracle, element by element
+within the oracle's bounds (what the roundings that the library names can make).
+lse is held in 32 bits: off by 2^-14 of the largest score's size (a score is a
+sum of at most 128 products, a sum of exponentials off by 2^-18)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import grouped
+from paper_2609_18145_amd import hcmix
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    hcmix.load()
+
+
+def draw(batch, n_q, n_k, heads, kv, hd, seed, size=1.0):
+    g = torch.Generator().manual_seed(seed)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=g).to(torch.bfloat16).cuda()
+    q, k = normal(batch, n_q, heads, hd) * size, normal(batch, n_k, kv, hd)
+    return q, k, normal(batch, n_k, kv, hd), normal(batch, n_q, heads, hd)
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def within(name, got, ref, bound):
+    err = np.abs(host(got) - ref)
+    with np.errstate(invalid="ignore", divide="ignore"):
+        print(f"  {name}: largest error {err.max():.2e}, of its bound {np.nanmax(err / bound):.2f}",
+              flush=True)
+    assert (err <= bound).all(), name
+
+
+def check(q, k, v, do, causal, lengths, scale=None, grads=True):
+    ln = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    out, lse = hcmix.grouped_attention_forward(q, k, v, causal, ln, scale)
+    hq, hk, hv, hdo = (host(t) for t in (q, k, v, do))
+    r_out, r_lse, bound = grouped.forward(hq, hk, hv, causal, lengths, scale)
+    within("out", out, r_out, bound)
+    empty = np.isneginf(r_lse)
+    assert np.array_equal(np.isneginf(host(lse)), empty)
+    top = max(1.0, np.abs(r_lse[~empty]).max(initial=0.0))
+    assert np.abs(host(lse)[~empty] - r_lse[~empty]).max(initial=0.0) <= 2.0 ** -14 * top
+    if not grads:
+        return out, lse
+    g = hcmix.grouped_attention_backward(q, k, v, out, lse, do, causal, ln, scale)
+    again = hcmix.grouped_attention_backward(q, k, v, out, lse, do, causal, ln, scale)
+    ref, bounds = grouped.backward(hq, hk, hv, hdo, causal, lengths, scale)
+    for i, name in enumerate(("dq", "dk", "dv")):
+        within(name, g[i], ref[i], bounds[i])
+        assert torch.equal(g[i], again[i])
+    return g
+
+
+# batch, n_q, n_k, heads, kv_heads, head_dim, causal, lengths, size of the queries
+CASES = [
+    (1, 1, 1, 1, 1, 64, True, None, 1.0), (2, 1, 300, 4, 2, 128, True, None, 1.0),
+    (2, 31, 31, 2, 2, 64, True, None, 1.0), (1, 32, 33, 3, 1, 128, False, None, 1.0),
+    (2, 64, 64, 2, 1, 64, False, None, 1.0), (1, 65, 129, 4, 4, 64, True, None, 1.0),
+    (2, 127, 257, 6, 2, 128, True, [257, 1], 1.0), (3, 128, 128, 2, 2, 64, True, [0, 5, 128], 1.0),
+    (1, 129, 65, 2, 1, 64, True, None, 1.0),      # the first 64 rows see nothing
+    (2, 200, 40, 2, 2, 128, True, [40, 7], 1.0), (3, 100, 100, 4, 1, 128, False, [0, 33, 100], 1.0),
+    (1, 513, 513, 2, 1, 64, True, None, 3.0), (1, 300, 700, 8, 1, 64, False, [650], 3.0),
+    (2, 1000, 1000, 2, 1, 128, True, [1000, 511], 1.0), (1, 4096, 40, 1, 1, 64, False, None, 1.0),
+    (1, 40, 4096, 1, 1, 128, True, None, 1.0), (2, 7, 7, 4, 4, 64, True, [-3, 99], 1.0),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "x".join(map(str, c[:6])))
+def test_matches_the_oracle(case):
+    print(f"case: grouped attention {case}", flush=True)
+    batch, n_q, n_k, heads, kv, hd, causal, lengths, size = case
+    check(*draw(batch, n_q, n_k, heads, kv, hd, seed=n_q + n_k, size=size), causal, lengths)
+
+
+def test_long_window_sampled():
+    """A sequence of 4096; the last head of the last group checked whole."""
+    q, k, v, do = draw(1, 4096, 4096, 4, 2, 64, seed=9)
+    out, lse = hcmix.grouped_attention_forward(q, k, v)
+    g = hcmix.grouped_attention_backward(q, k, v, out, lse, do)
+    s = [host(t) for t in (q[:, :, 2:], k[:, :, 1:], v[:, :, 1:], do[:, :, 2:])]
+    r_out, _, bound = grouped.forward(*s[:3])
+    within("out", out[:, :, 2:], r_out, bound)
+    ref, bounds = grouped.backward(*s)
+    for i, name in enumerate(("dq", "dk", "dv")):
+        within(name, g[i][:, :, 2 if i == 0 else 1:], ref[i], bounds[i])
+
+
+@pytest.mark.parametrize("heads,kv,hd", [(4, 2, 64), (2, 2, 128)])
+def test_packed_projection_in_and_out(heads, kv, hd):
+    """Slices of one packed buffer in and one packed gradient out: as apart."""
+    n = 70
+    g = torch.Generator().manual_seed(1)
+    packed = torch.randn((2, n, heads + 2 * kv, hd), generator=g).to(torch.bfloat16).cuda()
+    do = torch.randn((2, n, heads, hd), generator=g).to(torch.bfloat16).cuda()
+    q, k, v = packed.split([heads, kv, kv], 2)
+    out, lse = hcmix.grouped_attention_forward(q, k, v)
+    a = hcmix.grouped_attention_forward(q.contiguous(), k.contiguous(), v.contiguous())
+    assert torch.equal(out, a[0]) and torch.equal(lse, a[1])
+    dpacked = torch.full_like(packed, 3)
+    hcmix.grouped_attention_backward(q, k, v, out, lse, do,
+                                     **dict(zip(("dq", "dk", "dv"),
+                                                dpacked.split([heads, kv, kv], 2))))
+    b = hcmix.grouped_attention_backward(q.contiguous(), k.contiguous(), v.contiguous(), out, lse,
+                                         do)
+    assert torch.equal(dpacked, torch.cat(b, 2))
+
+
+@pytest.mark.parametrize("fill", [float("nan"), float("inf"), torch.finfo(torch.bfloat16).min])
+def test_what_lies_behind_the_lengths_is_not_taken(fill):
+    q, k, v, do = draw(2, 90, 90, 2, 1, 64, seed=3)
+    ln = torch.tensor([37, 64], dtype=torch.int32, device="cuda")
+    res = []
+    for put in (0.0, fill):
+        for b, n in enumerate((37, 64)):
+            k[b, n:], v[b, n:] = put, put
+        out, lse = hcmix.grouped_attention_forward(q, k, v, True, ln)
+        res.append((out, lse, *hcmix.grouped_attention_backward(q, k, v, out, lse, do, True, ln)))
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+    assert (res[1][3][0, 37:] == 0).all() and (res[1][4][1, 64:] == 0).all()
+
+
+def test_rows_do_not_see_ahead():
+    q, k, v, _ = draw(1, 300, 300, 2, 1, 128, seed=4)
+    a, la = hcmix.grouped_attention_forward(q, k, v)
+    for i in (0, 63, 64, 200):
+        k2, v2 = k.clone(), v.clone()
+        k2[:, i + 1:], v2[:, i + 1:] = 5.0, -3.0
+        b, lb = hcmix.grouped_attention_forward(q, k2, v2)
+        assert torch.equal(a[:, :i + 1], b[:, :i + 1])
+        assert torch.equal(la[:, :, :i + 1], lb[:, :, :i + 1])
+
+
+def test_other_scale_and_autograd():
+    q, k, v, do = draw(2, 50, 50, 4, 2, 64, seed=5)
+    leaves = [t.clone().requires_grad_(True) for t in (q, k, v)]
+    out = hcmix.GroupedAttention.apply(*leaves, True, None, 0.25)
+    out.backward(do)
+    ref, bounds = grouped.backward(*(host(t) for t in (q, k, v, do)), scale=0.25)
+    for i, t in enumerate(leaves):
+        within(f"grad {i}", t.grad, ref[i], bounds[i])
+
+
+def test_on_another_stream_and_captured():
+    q, k, v, do = draw(2, 130, 130, 4, 2, 64, seed=6)
+    out, lse = hcmix.grouped_attention_forward(q, k, v)
+    want = (out, lse, *hcmix.grouped_attention_backward(q, k, v, out, lse, do))
+
+    def step():
+        o, l = hcmix.grouped_attention_forward(q, k, v)
+        return (o, l, *hcmix.grouped_attention_backward(q, k, v, o, l, do))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(3):
+        for t in got:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -1,0 +1,131 @@
+"""Hybrid stacks whose attention layers go past the fixed windows: a training
+step with rotary positions and shared key/value heads against the oracle, and
+decoding position by position."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import grouped
+from oracle import hybrid as hybrid_oracle
+from paper_2609_18145_amd import hcmix, inputs
+from paper_2609_18145_amd.hybrid import HybridStack
+from tests.util import TOL, fro_rel_err, row_rel_err, to_dev, to_host
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    hcmix.load()
+
+
+def bf(rng, shape, scale=1.0):
+    return inputs.round_bf16((rng.standard_normal(shape) * scale).astype(np.float32))
+
+
+@pytest.mark.parametrize("batch,n,heads,kv,hd,layout", [(2, 64, 4, 2, 64, "half"),
+                                                        (1, 512, 2, 1, 128, "pairs"),
+                                                        (2, 16, 3, 3, 64, None)])
+def test_attention_segment_against_the_oracle(batch, n, heads, kv, hd, layout):
+    """One attention layer between sparse ones, forward and backward; the layer
+    is checked on the library's own input and output gradient, as the hybrids'
+    segments are, within the bf16 bound."""
+    print(f"case: hybrid {batch} {n} {heads} {kv} {hd} {layout}", flush=True)
+    width = heads * hd
+    s = inputs.make_stack(batch, n, width, 2, True, "bf16", seed=n)
+    rng = np.random.default_rng(n)
+    wqkv = bf(rng, ((heads + 2 * kv) * hd, width), 0.25 * width ** -0.5)
+    wout = bf(rng, (width, width), width ** -0.5)
+    freqs = hcmix.rotary_frequencies(hd)[0] if layout else None
+    h = HybridStack([0, "attn", 1], [to_dev(a, "bf16") for a in s.w_self],
+                    [to_dev(a, "bf16") for a in s.w_off],
+                    [(to_dev(wqkv, "bf16"), to_dev(wout, "bf16"))], heads, kv_heads=kv,
+                    rotary=dict(freqs=freqs, layout=layout) if layout else None)
+    xs = [to_dev(s.x, "bf16")]
+    for k in range(3):
+        xs.append(h.forward_segment(k, xs[-1]))
+    gs = [to_dev(s.dy, "bf16")]
+    h._dw_in, h.dw_attn = [], [None]
+    for k in (2, 1, 0):
+        gs.insert(0, h.backward_segment(k, gs[0]))
+    torch.cuda.synchronize()
+    x, dy = to_host(xs[1]).reshape(-1, width), to_host(gs[2]).reshape(-1, width)
+
+    def turn(t, inverse=False):
+        if layout:
+            t = t.copy()
+            t[:, :, :heads + kv] = grouped.rotary(t[:, :, :heads + kv], np.arange(n)[None],
+                                                  freqs.cpu().numpy(), layout == "half",
+                                                  inverse=inverse)
+        return t
+    packed = turn(hybrid_oracle.linear_forward(x, wqkv).reshape(batch, n, -1, hd))
+    q, k, v = np.split(packed, [heads, heads + kv], 2)
+    o = grouped.forward(q, k, v)[0].reshape(-1, width)
+    y = hybrid_oracle.linear_forward(o, wout)
+    d_o, d_wout = hybrid_oracle.linear_backward(o, wout, dy)
+    dq, dk, dv = grouped.backward(q, k, v, d_o.reshape(batch, n, heads, hd))[0]
+    dpacked = turn(np.concatenate([dq, dk, dv], 2), inverse=True).reshape(batch * n, -1)
+    dx, d_wqkv = hybrid_oracle.linear_backward(x, wqkv, dpacked)
+    errs = dict(y=row_rel_err(to_host(xs[2]).reshape(-1, width), y),
+                dx=row_rel_err(to_host(gs[1]).reshape(-1, width), dx),
+                dwqkv=fro_rel_err(to_host(h.dw_attn[0][0]), d_wqkv),
+                dwout=fro_rel_err(to_host(h.dw_attn[0][1]), d_wout))
+    print("  ", {a: f"{b:.2e}" for a, b in errs.items()}, flush=True)
+    assert max(errs.values()) <= TOL["bf16"], errs
+
+
+@pytest.mark.parametrize("batch,n,heads,kv,hd,rotary", [(3, 128, 4, 2, 64, True),
+                                                        (2, 64, 2, 2, 128, False),
+                                                        (1, 128, 1, 1, 64, True)])
+def test_decoding_against_the_cache_oracle(batch, n, heads, kv, hd, rotary):
+    """An attention layer with the identity behind it, position by position: its
+    outputs lie within the bounds of attention over what the oracle's cache holds
+    of the projections (made by the library for the whole window)."""
+    print(f"case: hybrid decode {batch} {n} {heads} {kv} {hd} {rotary}", flush=True)
+    width = heads * hd
+    rng = np.random.default_rng(heads)
+    x = to_dev(bf(rng, (batch, n, width)), "bf16")
+    wqkv = to_dev(bf(rng, ((heads + 2 * kv) * hd, width), width ** -0.5), "bf16")
+    freqs = hcmix.rotary_frequencies(hd)[0]
+    h = HybridStack(["attn"], [], [], [(wqkv, torch.eye(width, dtype=torch.bfloat16, device="cuda"))],
+                    heads, kv_heads=kv, rotary=dict(freqs=freqs) if rotary else None)
+    d = h.decoder(batch, n)
+    got = torch.stack([d.step(x[:, p].contiguous(), p) for p in range(n)], 1)
+    packed = hcmix.linear_forward(x.view(batch * n, width), wqkv).view(batch, n, -1, hd)
+    if rotary:
+        hcmix.rotary(packed[:, :, :heads + kv], freqs, out=packed[:, :, :heads + kv])
+    torch.cuda.synchronize()
+    q, k, v = (to_host(t) for t in packed.split([heads, kv, kv], 2))
+    caches = [[grouped.Cache(n, kv, hd) for _ in range(batch)] for _ in range(2)]
+    got = to_host(got).reshape(batch, n, heads, hd)
+    for p in range(n):
+        for b in range(batch):
+            for c, t in zip(caches, (k, v)):
+                c[b].append(t[b, p:p + 1], p)
+            r, _, bound = grouped.forward(q[b:b + 1, p:p + 1], caches[0][b].held[None, :p + 1],
+                                          caches[1][b].held[None, :p + 1])
+            assert (np.abs(got[b, p] - r[0, 0]) <= bound[0, 0]).all(), (b, p)
+
+
+def test_decoding_a_hybrid_follows_its_forward():
+    """Sparse layers and an attention layer: the sparse prefix equals the stack's
+    own decode, and the whole stays near the forward.  A held key or value is off by
+    2^-4 of itself at most, and evenly so: by 2^-4 / sqrt(3) = 0.036 in the mean square
+    at the worst place of a binade; a sum of such, and scores off by as much of
+    their size (here about 1/16), stay below 0.1 of the rows' norms."""
+    batch, n, width = 2, 64, 128
+    s = inputs.make_stack(batch, n, width, 4, True, "bf16", seed=2)
+    rng = np.random.default_rng(3)
+    attn = (to_dev(bf(rng, (3 * width, width), 0.25 * width ** -0.5), "bf16"),
+            to_dev(bf(rng, (width, width), width ** -0.5), "bf16"))
+    ws, wo = ([to_dev(a, "bf16") for a in t] for t in (s.w_self, s.w_off))
+    h = HybridStack([0, 1, "attn", 2, hcmix.LAYER_NEAR], ws, wo, [attn], 2)
+    x = to_dev(s.x, "bf16")
+    y = to_host(h.forward(x))
+    d = h.decoder(batch, n)
+    got = torch.stack([d.step(x[:, p].contiguous(), p) for p in range(n)], 1)
+    with pytest.raises(ValueError, match="pos"):
+        d.step(x[:, 0].contiguous(), n)
+    assert fro_rel_err(to_host(got), y) < 0.1

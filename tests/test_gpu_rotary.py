@@ -1,0 +1,108 @@
+"""Rotary positions against the oracle, element by element.
+
+An output is rounded once (bf16: half a step of 2^-8; fp32 2^-24) after products
+and a sum in 32 bits of (a, b) with a cosine and a sine; those are off by 2 pi
+2^-26 (the fraction of a turn, rounded to 32 bits) and 2^-23 (the functions): in
+all at most 2^-20 of scale (|a| + |b|)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import grouped
+from paper_2609_18145_amd import hcmix
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    hcmix.load()
+
+
+def check(y, x, positions, freqs, half, scale, inverse):
+    xs = x.double().cpu().numpy()
+    ref = grouped.rotary(xs, positions, freqs.cpu().numpy(), half, scale, inverse)
+    rot = 2 * len(freqs)
+    pair = np.zeros_like(xs)
+    ia = slice(0, rot // 2) if half else slice(0, rot, 2)
+    ib = slice(rot // 2, rot) if half else slice(1, rot, 2)
+    pair[..., ia] = pair[..., ib] = np.abs(xs[..., ia]) + np.abs(xs[..., ib])
+    u = 2.0 ** -8 if x.dtype == torch.bfloat16 else 2.0 ** -24
+    err = np.abs(y.double().cpu().numpy() - ref)
+    assert (err <= u * np.abs(ref) + 2.0 ** -20 * abs(scale) * pair).all(), err.max()
+    assert np.array_equal(y.double().cpu().numpy()[..., rot:], xs[..., rot:])
+
+
+# batch, n, heads, heads beside them in the packed rows, head_dim, rot_dim
+SHAPES = [(1, 1, 1, 0, 64, 64), (64, 1, 16, 8, 64, 64), (2, 37, 5, 1, 128, 96), (3, 5, 3, 0, 80, 48),
+          (2, 9, 2, 1, 34, 34), (1, 3, 7, 2, 10, 6), (2, 1030, 4, 0, 64, 32), (5, 7, 1, 0, 512, 512),
+          (1, 2, 1024, 0, 2, 2), (1, 17, 3, 0, 64, 2)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_rotary_matches_the_oracle(shape, layout, dtype):
+    print(f"case: rotary {shape} {layout} {dtype}", flush=True)
+    batch, n, heads, others, hd, rot = shape
+    g = torch.Generator().manual_seed(hd + heads)
+    packed = torch.randn((batch, n, heads + others, hd), generator=g).to(DT[dtype]).cuda()
+    x = packed[:, :, :heads]
+    freqs, _ = hcmix.rotary_frequencies(rot)
+    check(hcmix.rotary(x, freqs, layout=layout), x, np.arange(n)[None], freqs, layout == "half", 1.0,
+          False)
+    pos = torch.randint(-3000000, 3000000, (batch, n), generator=g, dtype=torch.int32)
+    for inverse in (False, True):
+        y = hcmix.rotary(x, freqs, pos.cuda(), layout, inverse, scale=1.25)
+        check(y, x, pos.numpy(), freqs, layout == "half", 1.25, inverse)
+    before = packed.clone()
+    into = torch.empty((batch, n, heads + 3, hd), dtype=x.dtype, device="cuda").fill_(7)
+    hcmix.rotary(x, freqs, pos.cuda(), layout, out=into[:, :, 1:heads + 1])   # strided, not packed alike
+    hcmix.rotary(x, freqs, pos.cuda(), layout, out=x)                         # in place
+    assert torch.equal(into[:, :, 1:heads + 1], x)
+    assert (into[:, :, 0] == 7).all() and (into[:, :, heads + 1:] == 7).all()
+    assert torch.equal(packed[:, :, heads:], before[:, :, heads:])
+    check(x, before[:, :, :heads], pos.numpy(), freqs, layout == "half", 1.0, False)
+
+
+@pytest.mark.parametrize("scaling", ["linear", "ntk", "yarn"])
+def test_scaled_contexts(scaling):
+    freqs, scale = hcmix.rotary_frequencies(64, scaling=scaling, factor=16.0, original_length=4096)
+    x = torch.randn(1, 8, 2, 64, device="cuda")
+    pos = torch.tensor([[0, 1, 4095, 4096, 65535, 65536, 1 << 24, (1 << 31) - 1]], dtype=torch.int32)
+    y = hcmix.rotary(x, freqs, pos.cuda(), scale=scale)
+    check(y, x, pos.numpy(), freqs, True, scale, False)
+
+
+def test_gradient_is_the_inverse_turn():
+    x = torch.randn(2, 5, 3, 64, device="cuda", requires_grad=True)
+    freqs, _ = hcmix.rotary_frequencies(64)
+    pos = torch.arange(10, dtype=torch.int32, device="cuda").view(2, 5)
+    gy = torch.randn_like(x)
+    y = hcmix.Rotary.apply(x, freqs, pos, "pairs", 0.5)
+    y.backward(gy)
+    check(x.grad, gy, pos.cpu().numpy(), freqs, False, 0.5, True)
+    # <R x, g> = <x, R^T g>, each a sum of 1920 terms of size 1 in 64 bits of values off by 2^-20
+    a, b = (y.double() * gy).sum(), (x.double() * x.grad).sum()
+    assert abs(a - b).item() < 1920 * 2.0 ** -18
+
+
+def test_captured_with_other_positions():
+    """A replay reads the positions that the buffer holds then."""
+    x = torch.randn(2, 3, 2, 64, device="cuda").to(torch.bfloat16)
+    freqs, _ = hcmix.rotary_frequencies(64)
+    pos = torch.zeros((2, 3), dtype=torch.int32, device="cuda")
+    out = torch.empty_like(x)
+    hcmix.rotary(x, freqs, pos, out=out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        hcmix.rotary(x, freqs, pos, out=out)
+    for p in (0, 5, 77):
+        pos.fill_(p)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, hcmix.rotary(x, freqs, pos))
