@@ -540,7 +540,7 @@ hcmix_status hcmix_head_cross_entropy(int64_t rows, int64_t width, int32_t vocab
  *
  * Activations are [batch][n][heads][head_dim]: a position's heads lie side by
  * side, and consecutive positions of the whole batch lie `stride` elements
- * apart (stride >= heads * head_dim; sequence b's position i is row b * n + i),
+ * apart (heads * head_dim <= stride <= 2^24; sequence b's position i is row b * n + i),
  * so that the queries, keys and values of one packed projection can be given
  * where they are.  Extents count the elements that are touched: an output may
  * lie between the rows of an input or of another output, with the same stride.
@@ -560,7 +560,7 @@ hcmix_status hcmix_head_cross_entropy(int64_t rows, int64_t width, int32_t vocab
  * outputs rounded once.  head_dim and rot_dim even, rot_dim <= head_dim <= 512,
  * heads <= 1024, rows <= 2^30.
  * HCMIX_ERR_INVALID_VALUE: null pointers, sizes or period < 1, sizes past those
- * bounds, strides below heads * head_dim, an unknown layout or dtype, a scale
+ * bounds, strides outside those bounds, an unknown layout or dtype, a scale
  * that is not finite, overlaps.  HCMIX_ERR_UNSUPPORTED: an odd head_dim or
  * rot_dim, pointers not aligned to an element (freqs: 8 bytes). */
 enum { HCMIX_ROTARY_HALF = 0, HCMIX_ROTARY_PAIRS = 1 };
@@ -587,7 +587,7 @@ hcmix_status hcmix_rotary(int64_t rows, int32_t heads, int32_t head_dim, int32_t
  * n_q, n_k <= 2^20, q_heads <= 1024, batch * n <= 2^30; scale positive, finite.
  * HCMIX_ERR_INVALID_VALUE: null pointers (lengths may be), sizes < 1 or past
  * those bounds, q_heads no multiple of kv_heads, causal not 0 or 1, a scale that
- * is not positive and finite, strides below heads * head_dim, overlaps.
+ * is not positive and finite, strides outside those bounds, overlaps.
  * HCMIX_ERR_UNSUPPORTED: another head_dim, strides that are no multiple of 8,
  * bf16 pointers not 16-byte, others not 4-byte aligned. */
 hcmix_status hcmix_grouped_attention_forward(
@@ -652,7 +652,7 @@ hcmix_status hcmix_grouped_attention_backward(
  * HCMIX_ERR_INVALID_VALUE: null pointers (counts may be), sizes < 1, batch above
  * 65535, capacity above 2^24, tokens above 2^16, heads above 1024, q_heads no
  * multiple of kv_heads, a cache shorter than the query, a scale that is not
- * positive and finite, strides below heads * head_dim, overlaps.
+ * positive and finite, strides outside those bounds, overlaps.
  * HCMIX_ERR_UNSUPPORTED: head_dim not 64 or 128, strides that are no multiple of
  * 8, bf16 pointers not 16-byte, the cache and workspace not 256-byte, others not
  * 4-byte aligned. */

@@ -1465,7 +1465,7 @@ Rows rows_of(const void* p, int64_t rows, int64_t stride, int64_t width, size_t 
   return Rows{p, (size_t)rows, (size_t)stride * elem, (size_t)width * elem};
 }
 
-constexpr int64_t kMaxStride = (int64_t)1 << 32;     // elements between two positions
+constexpr int64_t kMaxStride = (int64_t)1 << 24;     // elements between two positions
 
 bool positive(float v) { return v > 0.f && v <= 3.4028235e38f; }
 
@@ -1586,7 +1586,7 @@ size_t hcmix_grouped_attention_backward_workspace_bytes(int64_t batch, int64_t n
                                                         int32_t q_heads, int32_t kv_heads,
                                                         int32_t head_dim) {
   if (check_grouped(batch, n_q, n_k, q_heads, kv_heads, head_dim) != HCMIX_OK) return 0;
-  return grouped_workspace_bytes(batch, n_q, q_heads);
+  return grouped_workspace_bytes(batch, n_q, n_k, q_heads, kv_heads, head_dim);
 }
 
 hcmix_status hcmix_grouped_attention_backward(
@@ -1600,7 +1600,7 @@ hcmix_status hcmix_grouped_attention_backward(
   hcmix_status st = check_grouped(batch, n_q, n_k, q_heads, kv_heads, head_dim);
   if (st != HCMIX_OK) return st;
   if ((causal != 0 && causal != 1) || !positive(scale)) return HCMIX_ERR_INVALID_VALUE;
-  const size_t need = grouped_workspace_bytes(batch, n_q, q_heads);
+  const size_t need = grouped_workspace_bytes(batch, n_q, n_k, q_heads, kv_heads, head_dim);
   if (workspace_bytes < need) return HCMIX_ERR_INVALID_VALUE;
   const int64_t qw = (int64_t)q_heads * head_dim, kw = (int64_t)kv_heads * head_dim;
   const int64_t strides[6] = {q_stride, dq_stride, k_stride, v_stride, dk_stride, dv_stride};

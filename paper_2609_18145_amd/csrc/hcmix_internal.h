@@ -299,12 +299,14 @@ struct GroupedArgs {
   float* lse;
   const bf16* dout;            // null in the forward, as all below
   bf16 *dq, *dk, *dv;
-  float *row_sum, *row_lse;    // in the workspace
+  float *stats, *partial;      // in the workspace
   int64_t q_stride, k_stride, v_stride, dq_stride, dk_stride, dv_stride;
   int batch, n_q, n_k, q_heads, kv_heads, group, head_dim, causal;
+  int parts;                   // blocks that share a key tile of the backward
   float scale;
 };
-size_t grouped_workspace_bytes(int64_t batch, int64_t n_q, int32_t q_heads);
+size_t grouped_workspace_bytes(int64_t batch, int64_t n_q, int64_t n_k, int32_t q_heads,
+                               int32_t kv_heads, int32_t head_dim);
 hipError_t launch_grouped_forward(const GroupedArgs& a, hipStream_t st);
 hipError_t launch_grouped_backward(GroupedArgs a, void* workspace, hipStream_t st);
 

@@ -16,6 +16,7 @@
 #include "tile64.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace hcmix {
 
@@ -27,35 +28,48 @@ constexpr int GA_TILE = 64;         // rows of an LDS tile
 // Rows of a block (32 to a wave).
 constexpr int GA_ROWS = 128;
 
-template <int D>
+// A buffer's index known at compile time: its LDS addresses are then offsets in
+// the instructions, not a third of a turn's vector work.
+template <int I>
+using Const = std::integral_constant<int, I>;
+
+// Fragments of a tile of R rows.
+template <int R>
 __device__ __forceinline__ bf16x8 ga_frag(const bf16* t, int r0, int c0, int lane) {
-  return att_frag(t + (c0 >> 6) * GA_TILE * HD, r0, c0 & 63, lane);
+  return att_frag(t + (c0 >> 6) * R * HD, r0, c0 & 63, lane);
 }
-template <int D>
+template <int R>
 __device__ __forceinline__ bf16x8 ga_trfrag(const bf16* t, int k0, int c0, int lane) {
-  return att_trfrag(t + (c0 >> 6) * GA_TILE * HD, k0, c0 & 63, lane);
+  return att_trfrag(t + (c0 >> 6) * R * HD, k0, c0 & 63, lane);
 }
 
-// A tile's way from global memory through registers into LDS: rows row0 .. + 64
-// of an array with rows `stride` elements apart, of which those at `valid` and
-// behind are zeros, whatever memory holds there.
-template <int D>
-struct TileLoad {
-  static constexpr int PER = GA_TILE * D / 8 / GA_THREADS;   // 16-byte pieces per thread
-  u32x4 v[PER];
-  __device__ __forceinline__ void load(const bf16* base, size_t stride, int row0, int valid) {
-#pragma unroll
-    for (int j = 0; j < PER; j++) {
-      const int pi = threadIdx.x + GA_THREADS * j, r = pi / (D / 8), p = pi % (D / 8);
-      v[j] = u32x4{0, 0, 0, 0};
-      if (row0 + r < valid) v[j] = *(const u32x4*)(base + (size_t)(row0 + r) * stride + 8 * p);
-    }
+// A tile's way straight into LDS: rows row0 .. + R of an array with rows `stride`
+// elements apart; rows at `valid` and behind are copies of the last before it
+// (finite where the valid ones are: their P is 0).  A wave copies every fourth
+// piece of 8 rows by 64 columns, lane l the 16 bytes that the swizzle wants there.
+template <int D, int R>
+struct TileDma {
+  static constexpr int PER = D / 64 * R / 32;        // pieces of a wave
+  unsigned off[PER];                                 // source bytes from row row0
+  int wave, lane;
+  __device__ __forceinline__ unsigned at(int j, int last, unsigned stride) const {
+    const int blk = wave + 4 * j, r = blk % (R / 8) * 8 + (lane >> 3);
+    return 2 * ((unsigned)min(r, last) * stride + blk / (R / 8) * HD + 8 * ((lane & 7) ^ att_sw(r)));
   }
-  __device__ __forceinline__ void store(bf16* tile) const {
+  __device__ __forceinline__ TileDma(int w, int l, int64_t stride) : wave(w), lane(l) {
 #pragma unroll
-    for (int j = 0; j < PER; j++) {
-      const int pi = threadIdx.x + GA_THREADS * j, r = pi / (D / 8), p = pi % (D / 8);
-      *(u32x4*)(tile + (p >> 3) * GA_TILE * HD + att_off(r, 8 * (p & 7))) = v[j];
+    for (int j = 0; j < PER; j++) off[j] = at(j, R, (unsigned)stride);
+  }
+  __device__ __forceinline__ void load(const bf16* base, int64_t stride, int row0, int valid,
+                                       bf16* tile) const {
+    const bf16* src = uniform_base(base + (size_t)row0 * stride);
+    if (row0 + R <= valid) {
+#pragma unroll
+      for (int j = 0; j < PER; j++) dma16_at(src, off[j], tile + (wave + 4 * j) * 512);
+    } else {
+#pragma unroll
+      for (int j = 0; j < PER; j++)
+        dma16_at(src, at(j, valid - 1 - row0, (unsigned)stride), tile + (wave + 4 * j) * 512);
     }
   }
 };
@@ -103,6 +117,15 @@ __device__ __forceinline__ void ga_rows(bf16x8 (&f)[D / 16], const bf16* base, s
 // ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
+// A wave has 32 queries.  While the exponentials of one key tile run, the matrix
+// unit makes the scores of the next: the loop carries them (its last turn makes
+// some that nothing takes).  m grows only when a tile's largest score passes it
+// by more than GA_SLACK (in log2 units; P and l then stay below 2^GA_SLACK and
+// that times the number of keys, far from any limit), so that the rescaling of
+// what has been accumulated, and the exchange of the maximum between the two
+// lanes of a query, is a rare branch.
+constexpr float GA_SLACK = 8.f;
+
 template <int D>
 __global__ __launch_bounds__(GA_THREADS, 2) void ga_fwd_kernel(GroupedArgs a, int total) {
   __shared__ __attribute__((aligned(1024))) bf16 sK[2][GA_TILE * D], sV[2][GA_TILE * D];
@@ -115,83 +138,96 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_fwd_kernel(GroupedArgs a, in
   const bf16* qb = a.q + (size_t)it.b * a.n_q * a.q_stride + (size_t)it.h * D;
   const bf16* kb = a.k + (size_t)it.b * a.n_k * a.k_stride + (size_t)kvh * D;
   const bf16* vb = a.v + (size_t)it.b * a.n_k * a.v_stride + (size_t)kvh * D;
-  // keys that the block's last query, and this wave's, sees
+  // keys that the block's last query, and this wave's, sees; keys that all of its do
   const int blk_end = a.causal ? min(len, blk0 + GA_ROWS + off) : len;
   const int wave_end = a.causal ? min(len, q0 + 32 + off) : len;
-  const int full_end = a.causal ? min(len, q0 + 1 + off) : len;   // seen by all of its queries
+  const int full_end = a.causal ? min(len, q0 + 1 + off) : len;
   const int tiles = blk_end > 0 ? (blk_end + GA_TILE - 1) / GA_TILE : 0;
+  const int mine = q0 < a.n_q && wave_end > 0 ? (wave_end + GA_TILE - 1) / GA_TILE : 0;
   bf16x8 qf[D / 16];
   ga_rows<D>(qf, qb, a.q_stride, q0, a.n_q, lane);
   f32x16 o[D / 32] = {};
-  float m = -3e38f, l = 0.f;
   const float sc = a.scale * GA_LOG2E;
-  TileLoad<D> lk, lv;
-  if (tiles) {
-    lk.load(kb, a.k_stride, 0, len);
-    lv.load(vb, a.v_stride, 0, len);
-    lk.store(sK[0]);
-    lv.store(sV[0]);
-  }
-  for (int t = 0; t < tiles; t++) {
-    __syncthreads();
-    if (t + 1 < tiles) {
-      lk.load(kb, a.k_stride, (t + 1) * GA_TILE, len);
-      lv.load(vb, a.v_stride, (t + 1) * GA_TILE, len);
+  float m = -3e38f, l = 0.f, limit = -INFINITY;      // limit: the score from which m grows
+  const TileDma<D, GA_TILE> dk(wave, lane, a.k_stride), dv(wave, lane, a.v_stride);
+  auto scores = [&](const bf16* tk, f32x16 (&r)[2]) {
+#pragma unroll
+    for (int kt = 0; kt < 2; kt++) {
+      r[kt] = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ks++)
+        r[kt] = mfma32(ga_frag<GA_TILE>(tk, 32 * kt, 16 * ks, lane), qf[ks], r[kt]);
     }
-    const bf16 *tk = sK[t & 1], *tv = sV[t & 1];
+  };
+  auto turn = [&](auto buf, int t, f32x16 (&s)[2], f32x16 (&next)[2]) {   // buf: t % 2
+    wait_dma();
+    __syncthreads();
+    if (t + 2 < tiles) dk.load(kb, a.k_stride, (t + 2) * GA_TILE, len, sK[buf]);
+    if (t + 1 < tiles) dv.load(vb, a.v_stride, (t + 1) * GA_TILE, len, sV[buf ^ 1]);
+    if (t >= mine) return;               // wave-uniform
     const int k0 = t * GA_TILE;
-    if (k0 < wave_end) {             // wave-uniform
-      f32x16 s[2];
-#pragma unroll
-      for (int kt = 0; kt < 2; kt++) {
-        s[kt] = f32x16{};
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ks++)
-          s[kt] = mfma32(ga_frag<D>(tk, 32 * kt, 16 * ks, lane), qf[ks], s[kt]);
-      }
-      if (k0 + GA_TILE > full_end) {
-        // register e of a lane: key k0 + 32 kt + 8 (e / 4) + 4 half + e % 4
-        const int end = a.causal ? min(len, q0 + (lane & 31) + 1 + off) : len;
-#pragma unroll
-        for (int kt = 0; kt < 2; kt++)
-#pragma unroll
-          for (int e = 0; e < 16; e++)
-            if (k0 + 32 * kt + 8 * (e >> 2) + 4 * half + (e & 3) >= end) s[kt][e] = -INFINITY;
-      }
-      float mx = s[0][0];
+    if (k0 + GA_TILE > full_end) {
+      asm volatile("; tile with keys that some query does not see");   // no selects elsewhere
+      // register e of a lane: key k0 + 32 kt + 8 (e / 4) + 4 half + e % 4
+      const int end = (a.causal ? min(len, q0 + (lane & 31) + 1 + off) : len) - k0 - 4 * half;
 #pragma unroll
       for (int kt = 0; kt < 2; kt++)
 #pragma unroll
-        for (int e = 0; e < 16; e++) mx = fmaxf(mx, s[kt][e]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32)) * sc;
-      const float mn = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - mn);
+        for (int e = 0; e < 16; e++)
+          if (32 * kt + 8 * (e >> 2) + (e & 3) >= end) s[kt][e] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) mx = fmaxf(mx, s[kt][e]);
+    if (__any(mx > limit)) {
+      const float mn = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32)) * sc);
+      const float alpha = __builtin_amdgcn_exp2f(m - mn);
       m = mn;
+      limit = (mn + GA_SLACK) / sc;
       l *= alpha;
 #pragma unroll
       for (int d = 0; d < D / 32; d++)
 #pragma unroll
         for (int e = 0; e < 16; e++) o[d][e] *= alpha;
-#pragma unroll
-      for (int kt = 0; kt < 2; kt++)
-#pragma unroll
-        for (int e = 0; e < 16; e++) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[kt][e], sc, -m));
-          s[kt][e] = p;
-          l += p;
-        }
-#pragma unroll
-      for (int kt = 0; kt < 2; kt++)
-#pragma unroll
-        for (int mm = 0; mm < 2; mm++) {
-          const bf16x8 pf = att_pack(s[kt], mm);
-#pragma unroll
-          for (int d = 0; d < D / 32; d++)
-            o[d] = mfma32(ga_trfrag<D>(tv, 32 * kt + 16 * mm, 32 * d, lane), pf, o[d]);
-        }
     }
-    if (t + 1 < tiles) {
-      lk.store(sK[(t + 1) & 1]);
-      lv.store(sV[(t + 1) & 1]);
+    scores(sK[buf ^ 1], next);
+    // of what follows, seven vector instructions to each of the matrix unit's
+#pragma unroll
+    for (int i = 0; i < D / 4; i++) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
+    }
+    const bf16* tv = sV[buf];
+#pragma unroll
+    for (int kt = 0; kt < 2; kt++) {
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[kt][e], sc, -m));
+        s[kt][e] = p;
+        l += p;
+      }
+#pragma unroll
+      for (int mm = 0; mm < 2; mm++) {
+        const bf16x8 pf = att_pack(s[kt], mm);
+#pragma unroll
+        for (int d = 0; d < D / 32; d++)
+          o[d] = mfma32(ga_trfrag<GA_TILE>(tv, 32 * kt + 16 * mm, 32 * d, lane), pf, o[d]);
+      }
+    }
+  };
+  if (tiles) {
+    f32x16 s[2], next[2];
+    dk.load(kb, a.k_stride, 0, len, sK[0]);
+    dv.load(vb, a.v_stride, 0, len, sV[0]);
+    if (tiles > 1) dk.load(kb, a.k_stride, GA_TILE, len, sK[1]);
+    wait_dma();
+    __syncthreads();
+    scores(sK[0], s);
+    for (int t = 0; t < tiles; t += 2) {
+      turn(Const<0>(), t, s, next);
+      if (t + 1 < tiles) turn(Const<1>(), t + 1, next, s);
     }
   }
   if (q0 >= a.n_q) return;
@@ -207,178 +243,297 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_fwd_kernel(GroupedArgs a, in
 }
 
 // ---------------------------------------------------------------------------
-// Backward.  A row's D and its lse in log2 units go to the workspace first, rows
-// padded to a multiple of 64: behind the last row, and for rows that see
-// nothing, an lse of +inf, which makes their P = 0.
+// Backward, in two kernels: dQ by query tiles, dK and dV by key tiles, each
+// making S and dP again (7 products of the 5 that one would need with atomics on
+// dQ, whose order changes results).  Both stream tiles of 32 rows through four
+// buffers in LDS, three ahead, and carry the next tile's S and dP while the
+// vector unit works on this one's.
+//
+// With lanes and registers as in the forward, S and dP start from -lse / scale
+// and -D instead of 0, so that P = exp2(S scale log2 e) and dS = P dP need no
+// subtraction.  A row that sees nothing starts from -inf: its P is 0.
 //
 // D = sum_j P_j dP_j = dout . out.  The second form is one pass over two rows,
 // but out is rounded to bf16, and dS = P (dP - D) cancels the more the fewer keys
 // share a row: a row that sees one key has dS = 0, and got 2^-9 |dout| |out|
 // instead (dq and dk of windows of 10 keys were 0.0046 off in all, 0.0024 so).
-// So tiles whose rows see at most GA_EXACT_KEYS keys take the first form, P and
-// dP made as in the kernels below; with more, the rounding of out adds less than
-// a tenth to that of dS.
+// So tiles whose rows see at most GA_EXACT_KEYS keys take the first form; with
+// more, the rounding of out adds less than a tenth to that of dS.
 // ---------------------------------------------------------------------------
 constexpr int GA_EXACT_KEYS = 128;
+constexpr int GA_STEP = 32;         // rows of a streamed tile
+constexpr int GA_BUFS = 4;
 
-template <int D>
-__global__ __launch_bounds__(GA_THREADS) void ga_row_sum_kernel(GroupedArgs a, int pad, int total) {
-  const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int item = blockIdx.x * (GA_THREADS / 64) + wave_index<GA_THREADS / 64>();
-  if (item >= total) return;
-  const int tiles = pad / 32, bh = item / tiles, q0 = (item - bh * tiles) * 32;
-  const int b = bh / a.q_heads, h = bh - b * a.q_heads;
-  const int len = ga_length(a, b), off = a.n_k - a.n_q;
-  const int end = a.causal ? min(len, q0 + 32 + off) : len;
-  const size_t os = (size_t)a.q_heads * D, row = (size_t)bh * pad + q0;
-  const bf16* dob = a.dout + (size_t)b * a.n_q * os + (size_t)h * D;
-  const float* lse = a.lse + (size_t)bh * a.n_q;
-  float l = INFINITY;              // of row lane % 32
-  if (q0 + (lane & 31) < a.n_q) {
-    l = lse[q0 + (lane & 31)];
-    l = l == -INFINITY ? INFINITY : l * GA_LOG2E;
-  }
-  if (half == 0) a.row_lse[row + lane] = l;
-  if (end <= GA_EXACT_KEYS) {      // wave-uniform
-    const bf16* kb = a.k + (size_t)b * a.n_k * a.k_stride + (size_t)(h / a.group) * D;
-    const bf16* vb = a.v + (size_t)b * a.n_k * a.v_stride + (size_t)(h / a.group) * D;
-    bf16x8 qf[D / 16], of[D / 16];
-    ga_rows<D>(qf, a.q + (size_t)b * a.n_q * a.q_stride + (size_t)h * D, a.q_stride, q0, a.n_q, lane);
-    ga_rows<D>(of, dob, os, q0, a.n_q, lane);
-    const int seen = a.causal ? min(len, q0 + (lane & 31) + 1 + off) : len;
-    float d = 0.f;
-    for (int k0 = 0; k0 < end; k0 += 32) {
-      bf16x8 kf[D / 16], vf[D / 16];
-      ga_rows<D>(kf, kb, a.k_stride, k0, len, lane);
-      ga_rows<D>(vf, vb, a.v_stride, k0, len, lane);
-      f32x16 s = {}, dp = {};
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ks++) {
-        s = mfma32(kf[ks], qf[ks], s);
-        dp = mfma32(vf[ks], of[ks], dp);
-      }
-#pragma unroll
-      for (int e = 0; e < 16; e++) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale * GA_LOG2E, -l));
-        d += k0 + 8 * (e >> 2) + 4 * half + (e & 3) < seen ? p * dp[e] : 0.f;
-      }
-    }
-    d += __shfl_xor(d, 32);
-    if (half == 0) a.row_sum[row + lane] = d;
-    return;
-  }
-  constexpr int PER = D / 8, RW = 64 / PER;      // lanes of a row, rows at a time
-  const int piece = lane % PER;
-#pragma unroll
-  for (int r0 = 0; r0 < 32; r0 += RW) {
-    const int r = r0 + lane / PER;
-    float d = 0.f;
-    if (q0 + r < a.n_q) {
-      const bf16x8 y = *(const bf16x8*)(dob + (size_t)(q0 + r) * os + 8 * piece);
-      const bf16x8 x = *(const bf16x8*)(a.out + ((size_t)b * a.n_q + q0 + r) * os + (size_t)h * D + 8 * piece);
-#pragma unroll
-      for (int e = 0; e < 8; e++) d += (float)x[e] * (float)y[e];
-    }
-#pragma unroll
-    for (int s = 1; s < PER; s *= 2) d += __shfl_xor(d, s);
-    if (piece == 0) a.row_sum[row + r] = d;
-  }
+// What the dQ kernel leaves for the other, for each head and 32 rows: 32 of
+// -lse / scale, then 32 of -D.
+__device__ __forceinline__ size_t ga_stats(int bh, int n_q, int row0) {
+  return ((size_t)bh * ((n_q + 31) / 32) + row0 / 32) * 64;
 }
 
-// dK and dV of 128 keys of one key/value head: over the group's query heads and
-// the query tiles that see them, S and dP with lanes = keys.
+template <int D>
+__global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a, int total) {
+  __shared__ __attribute__((aligned(1024))) bf16 sK[GA_BUFS][GA_STEP * D], sV[GA_BUFS][GA_STEP * D];
+  Item it;
+  if (!ga_item(a.q_heads, (a.n_q + GA_ROWS - 1) / GA_ROWS, total, a.causal, &it)) return;
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = wave_index<GA_THREADS / 64>();
+  const int kvh = it.h / a.group, len = ga_length(a, it.b), off = a.n_k - a.n_q;
+  const int blk0 = it.tile * GA_ROWS, q0 = blk0 + 32 * wave;
+  const size_t os = (size_t)a.q_heads * D;
+  const bf16* kb = a.k + (size_t)it.b * a.n_k * a.k_stride + (size_t)kvh * D;
+  const bf16* vb = a.v + (size_t)it.b * a.n_k * a.v_stride + (size_t)kvh * D;
+  const int blk_end = a.causal ? min(len, blk0 + GA_ROWS + off) : len;
+  const int wave_end = a.causal ? min(len, q0 + 32 + off) : len;
+  const int full_end = a.causal ? min(len, q0 + 1 + off) : len;
+  const int tiles = blk_end > 0 ? (blk_end + GA_STEP - 1) / GA_STEP : 0;
+  const int mine = q0 < a.n_q && wave_end > 0 ? (wave_end + GA_STEP - 1) / GA_STEP : 0;
+  const TileDma<D, GA_STEP> dk(wave, lane, a.k_stride), dv(wave, lane, a.v_stride);
+  auto load = [&](auto buf, int t) {      // buf: t % GA_BUFS
+    if (t >= tiles) return;
+    dk.load(kb, a.k_stride, t * GA_STEP, len, sK[buf]);
+    dv.load(vb, a.v_stride, t * GA_STEP, len, sV[buf]);
+  };
+  load(Const<0>(), 0);
+  load(Const<1>(), 1);
+  load(Const<2>(), 2);
+  bf16x8 qf[D / 16], of[D / 16];
+  ga_rows<D>(qf, a.q + (size_t)it.b * a.n_q * a.q_stride + (size_t)it.h * D, a.q_stride, q0, a.n_q, lane);
+  ga_rows<D>(of, a.dout + (size_t)it.b * a.n_q * os + (size_t)it.h * D, os, q0, a.n_q, lane);
+  const float sc = a.scale * GA_LOG2E;
+  // keys that this lane's query sees, and its statistics
+  const int seen = a.causal ? min(len, q0 + (lane & 31) + 1 + off) : len;
+  float start = -INFINITY, d = 0.f;
+  if (q0 < a.n_q) {                       // wave-uniform
+    if (q0 + (lane & 31) < a.n_q) {
+      const float lse = a.lse[((size_t)it.b * a.q_heads + it.h) * a.n_q + q0 + (lane & 31)];
+      start = lse == -INFINITY ? -INFINITY : -lse / a.scale;
+    }
+    if (wave_end <= GA_EXACT_KEYS) {      // wave-uniform
+      for (int k0 = 0; k0 < wave_end; k0 += 32) {
+        bf16x8 kf[D / 16], vf[D / 16];
+        ga_rows<D>(kf, kb, a.k_stride, k0, len, lane);
+        ga_rows<D>(vf, vb, a.v_stride, k0, len, lane);
+        f32x16 s = {}, dp = {};
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ks++) {
+          s = mfma32(kf[ks], qf[ks], s);
+          dp = mfma32(vf[ks], of[ks], dp);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+          const float p = __builtin_amdgcn_exp2f((s[e] + start) * sc);
+          d += k0 + 8 * (e >> 2) + 4 * half + (e & 3) < seen ? p * dp[e] : 0.f;
+        }
+      }
+    } else {
+      bf16x8 xf[D / 16];
+      ga_rows<D>(xf, a.out + (size_t)it.b * a.n_q * os + (size_t)it.h * D, os, q0, a.n_q, lane);
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ks++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) d += (float)xf[ks][e] * (float)of[ks][e];
+    }
+    d += __shfl_xor(d, 32);
+    a.stats[ga_stats(it.b * a.q_heads + it.h, a.n_q, q0) + lane] = half ? -d : start;
+  }
+  f32x16 start16, d16;
+#pragma unroll
+  for (int e = 0; e < 16; e++) {
+    start16[e] = start;
+    d16[e] = -d;
+  }
+  f32x16 gq[D / 32] = {};
+  auto scores = [&](auto buf, f32x16& s, f32x16& dp) {
+    const bf16 *tk = sK[buf], *tv = sV[buf];
+    s = start16;
+    dp = d16;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ks++) {
+      s = mfma32(ga_frag<GA_STEP>(tk, 0, 16 * ks, lane), qf[ks], s);
+      dp = mfma32(ga_frag<GA_STEP>(tv, 0, 16 * ks, lane), of[ks], dp);
+    }
+  };
+  auto turn = [&](auto buf, int t, f32x16& s, f32x16& dp, f32x16& s_next, f32x16& dp_next) {
+    // tile t + 1 has landed when at most t + 2's loads are on their way
+    if (t + 2 < tiles) wait_vmcnt<2 * TileDma<D, GA_STEP>::PER>();
+    else wait_vmcnt<0>();
+    __syncthreads();
+    load(Const<(buf + 3) % GA_BUFS>(), t + 3);
+    if (t >= mine) return;                // wave-uniform
+    if ((t + 1) * GA_STEP > full_end) {
+      asm volatile("; tile with keys that some query does not see");   // no selects elsewhere
+#pragma unroll
+      for (int e = 0; e < 16; e++)
+        if (t * GA_STEP + 8 * (e >> 2) + 4 * half + (e & 3) >= seen) s[e] = -INFINITY;
+    }
+    scores(Const<(buf + 1) % GA_BUFS>(), s_next, dp_next);
+#pragma unroll
+    for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(s[e] * sc) * dp[e];
+    const bf16* tk = sK[buf];
+#pragma unroll
+    for (int mm = 0; mm < 2; mm++) {
+      const bf16x8 sf = att_pack(s, mm);
+#pragma unroll
+      for (int dt = 0; dt < D / 32; dt++)
+        gq[dt] = mfma32(ga_trfrag<GA_STEP>(tk, 16 * mm, 32 * dt, lane), sf, gq[dt]);
+    }
+#pragma unroll
+    for (int i = 0; i < 3 * D / 16; i++) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+    }
+  };
+  if (tiles) {
+    f32x16 s, dp, s2, dp2;
+    wait_vmcnt<0>();
+    __syncthreads();
+    scores(Const<0>(), s, dp);
+    for (int t = 0; t < tiles; t += 4) {
+      turn(Const<0>(), t, s, dp, s2, dp2);
+      if (t + 1 < tiles) turn(Const<1>(), t + 1, s2, dp2, s, dp);
+      if (t + 2 < tiles) turn(Const<2>(), t + 2, s, dp, s2, dp2);
+      if (t + 3 < tiles) turn(Const<3>(), t + 3, s2, dp2, s, dp);
+    }
+  }
+  if (q0 >= a.n_q) return;
+  bf16* dqb = a.dq + ((size_t)it.b * a.n_q + q0) * a.dq_stride + (size_t)it.h * D;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++)
+    att_store(dqb + 32 * dt, a.dq_stride, gq[dt], a.scale, lane, a.n_q - q0);
+}
+
+// dK and dV of 128 keys of one key/value head, S and dP with lanes = keys, over
+// the query tiles that see them of the group's heads one after the other.  Where
+// the key tiles are too few for the chip, a.parts blocks share that sequence of
+// query tiles and leave fp32 sums, which ga_join_kernel adds in order.
 template <int D>
 __global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(GroupedArgs a,
                                                                                 int total) {
-  __shared__ __attribute__((aligned(1024))) bf16 sQ[2][GA_TILE * D], sO[2][GA_TILE * D];
-  __shared__ __attribute__((aligned(16))) float sL[2][GA_TILE], sD[2][GA_TILE];
+  __shared__ __attribute__((aligned(1024))) bf16 sQ[GA_BUFS][GA_STEP * D], sO[GA_BUFS][GA_STEP * D];
+  // a tile's statistics, four times over: every wave copies them, to keep one
+  // count of loads on their way, and 64 lanes copy 1 KB
+  __shared__ __attribute__((aligned(1024))) float sS[GA_BUFS][256];
   Item it;
-  if (!ga_item(a.kv_heads, (a.n_k + GA_ROWS - 1) / GA_ROWS, total, false, &it)) return;
+  const int key_tiles = (a.n_k + GA_ROWS - 1) / GA_ROWS;
+  if (!ga_item(a.kv_heads, key_tiles * a.parts, total, false, &it)) return;
+  const int part = it.tile % a.parts;
+  it.tile /= a.parts;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = wave_index<GA_THREADS / 64>();
   const int len = ga_length(a, it.b), off = a.n_k - a.n_q;
-  const int blk0 = it.tile * GA_ROWS, j0 = blk0 + 32 * wave;
-  const int pad = (a.n_q + GA_TILE - 1) / GA_TILE * GA_TILE;
-  const bf16* kb = a.k + (size_t)it.b * a.n_k * a.k_stride + (size_t)it.h * D;
-  const bf16* vb = a.v + (size_t)it.b * a.n_k * a.v_stride + (size_t)it.h * D;
+  const int blk0 = it.tile * GA_ROWS, j0 = blk0 + 32 * wave, j = j0 + (lane & 31);
+  const size_t os = (size_t)a.q_heads * D;
   bf16x8 kf[D / 16], vf[D / 16];
-  ga_rows<D>(kf, kb, a.k_stride, j0, len, lane);
-  ga_rows<D>(vf, vb, a.v_stride, j0, len, lane);
+  ga_rows<D>(kf, a.k + (size_t)it.b * a.n_k * a.k_stride + (size_t)it.h * D, a.k_stride, j0, len, lane);
+  ga_rows<D>(vf, a.v + (size_t)it.b * a.n_k * a.v_stride + (size_t)it.h * D, a.v_stride, j0, len, lane);
   f32x16 dk[D / 32] = {}, dv[D / 32] = {};
   const float sc = a.scale * GA_LOG2E;
-  const size_t os = (size_t)a.q_heads * D;
-  // the first query tile that sees any of the block's keys
-  const int first = a.causal && blk0 - off > 0 ? (blk0 - off) / GA_TILE : 0;
-  const int per = blk0 < len ? max(0, pad / GA_TILE - first) : 0, steps = per * a.group;
-  TileLoad<D> lq, lo;
-  float rl = 0.f, rd = 0.f;
-  auto load = [&](int step) {
-    const int g = step / per, i0 = (first + step - g * per) * GA_TILE, h = it.h * a.group + g;
-    lq.load(a.q + (size_t)it.b * a.n_q * a.q_stride + (size_t)h * D, a.q_stride, i0, a.n_q);
-    lo.load(a.dout + (size_t)it.b * a.n_q * os + (size_t)h * D, os, i0, a.n_q);
-    const size_t row = ((size_t)it.b * a.q_heads + h) * pad + i0 + lane;
-    if (wave == 0) rl = a.row_lse[row];
-    if (wave == 1) rd = a.row_sum[row];
+  // the query tiles that see any of the block's keys: `per` of each head from
+  // `first` on; this block's are steps lo .. hi - 1 of them all
+  const int first = a.causal && blk0 - off > 0 ? (blk0 - off) / GA_STEP : 0;
+  const int per = blk0 < len ? max(0, (a.n_q + GA_STEP - 1) / GA_STEP - first) : 0;
+  const int lo = (int)((int64_t)per * a.group * part / a.parts);
+  const int steps = (int)((int64_t)per * a.group * (part + 1) / a.parts) - lo;
+  const TileDma<D, GA_STEP> dq(wave, lane, a.q_stride), dout(wave, lane, os);
+  int lg = steps ? lo / per : 0, lt = lo - lg * per;      // head and tile to be loaded next
+  int ct = lt;                                            // tile to be computed next
+  auto load = [&](auto buf, int step) {                   // buf: step % GA_BUFS
+    if (step >= steps) return;
+    const int h = it.h * a.group + lg, i0 = (first + lt) * GA_STEP;
+    dq.load(a.q + (size_t)it.b * a.n_q * a.q_stride + (size_t)h * D, a.q_stride, i0, a.n_q, sQ[buf]);
+    dout.load(a.dout + (size_t)it.b * a.n_q * os + (size_t)h * D, os, i0, a.n_q, sO[buf]);
+    dma16_at((const bf16*)(a.stats + ga_stats(it.b * a.q_heads + h, a.n_q, i0)), 16 * (lane & 15),
+             (bf16*)sS[buf]);
+    if (++lt == per) {
+      lt = 0;
+      lg++;
+    }
   };
-  auto store = [&](int buf) {
-    lq.store(sQ[buf]);
-    lo.store(sO[buf]);
-    if (wave == 0) sL[buf][lane] = rl;
-    if (wave == 1) sD[buf][lane] = rd;
-  };
-  if (steps) {
-    load(0);
-    store(0);
-  }
-  for (int step = 0; step < steps; step++) {
-    __syncthreads();
-    if (step + 1 < steps) load(step + 1);
-    const int buf = step & 1, i0 = (first + step % per) * GA_TILE;
+  auto scores = [&](auto buf, f32x16& s, f32x16& dp) {
     const bf16 *tq = sQ[buf], *to = sO[buf];
+    // register e: query 8 (e / 4) + 4 half + e % 4 of the tile, key j
 #pragma unroll
-    for (int qt = 0; qt < 2; qt++) {
-      const int r0 = i0 + 32 * qt;
-      if (j0 >= len || (a.causal && r0 + 31 + off < j0)) continue;     // wave-uniform
-      f32x16 s = {}, dp = {};
+    for (int g = 0; g < 4; g++) {
+      const f32x4 l4 = *(const f32x4*)(sS[buf] + 8 * g + 4 * half);
+      const f32x4 d4 = *(const f32x4*)(sS[buf] + 32 + 8 * g + 4 * half);
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ks++) {
-        s = mfma32(ga_frag<D>(tq, 32 * qt, 16 * ks, lane), kf[ks], s);
-        dp = mfma32(ga_frag<D>(to, 32 * qt, 16 * ks, lane), vf[ks], dp);
-      }
-      // register e: query r0 + 8 (e / 4) + 4 half + e % 4, key j0 + lane % 32
-#pragma unroll
-      for (int g = 0; g < 4; g++) {
-        const f32x4 l4 = *(const f32x4*)(sL[buf] + 32 * qt + 8 * g + 4 * half);
-#pragma unroll
-        for (int r = 0; r < 4; r++)
-          s[4 * g + r] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + r], sc, -l4[r]));
-      }
-      if (j0 + 32 > len || (a.causal && r0 + off < j0 + 31)) {
-        const int j = j0 + (lane & 31);
-        const int from = j >= len ? 1 << 30 : a.causal ? j - off - r0 : -1;   // first row that sees it
-#pragma unroll
-        for (int e = 0; e < 16; e++)
-          if (8 * (e >> 2) + 4 * half + (e & 3) < from) s[e] = 0.f;
-      }
-#pragma unroll
-      for (int g = 0; g < 4; g++) {
-        const f32x4 d4 = *(const f32x4*)(sD[buf] + 32 * qt + 8 * g + 4 * half);
-#pragma unroll
-        for (int r = 0; r < 4; r++) dp[4 * g + r] = s[4 * g + r] * (dp[4 * g + r] - d4[r]);
-      }
-#pragma unroll
-      for (int mm = 0; mm < 2; mm++) {
-        const bf16x8 pf = att_pack(s, mm), sf = att_pack(dp, mm);
-#pragma unroll
-        for (int d = 0; d < D / 32; d++) {
-          dv[d] = mfma32(ga_trfrag<D>(to, 32 * qt + 16 * mm, 32 * d, lane), pf, dv[d]);
-          dk[d] = mfma32(ga_trfrag<D>(tq, 32 * qt + 16 * mm, 32 * d, lane), sf, dk[d]);
-        }
+      for (int r = 0; r < 4; r++) {
+        s[4 * g + r] = l4[r];
+        dp[4 * g + r] = d4[r];
       }
     }
-    if (step + 1 < steps) store((step + 1) & 1);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ks++) {
+      s = mfma32(ga_frag<GA_STEP>(tq, 0, 16 * ks, lane), kf[ks], s);
+      dp = mfma32(ga_frag<GA_STEP>(to, 0, 16 * ks, lane), vf[ks], dp);
+    }
+  };
+  auto turn = [&](auto buf, int step, f32x16& s, f32x16& dp, f32x16& s_next, f32x16& dp_next) {
+    if (step + 2 < steps) wait_vmcnt<2 * TileDma<D, GA_STEP>::PER + 1>();
+    else wait_vmcnt<0>();
+    __syncthreads();
+    load(Const<(buf + 3) % GA_BUFS>(), step + 3);
+    const int r0 = (first + ct) * GA_STEP;
+    if (++ct == per) ct = 0;
+    if (j0 + 32 > len || (a.causal && r0 + off < j0 + 31)) {
+      asm volatile("; tile with keys that some query does not see");
+      const int from = j >= len ? 1 << 30 : a.causal ? j - off - r0 : -1;   // first row that sees j
+#pragma unroll
+      for (int e = 0; e < 16; e++)
+        if (8 * (e >> 2) + 4 * half + (e & 3) < from) s[e] = -INFINITY;
+    }
+    scores(Const<(buf + 1) % GA_BUFS>(), s_next, dp_next);
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+      s[e] = __builtin_amdgcn_exp2f(s[e] * sc);
+      dp[e] *= s[e];
+    }
+    const bf16 *tq = sQ[buf], *to = sO[buf];
+#pragma unroll
+    for (int mm = 0; mm < 2; mm++) {
+      const bf16x8 pf = att_pack(s, mm), sf = att_pack(dp, mm);
+#pragma unroll
+      for (int d = 0; d < D / 32; d++) {
+        dv[d] = mfma32(ga_trfrag<GA_STEP>(to, 16 * mm, 32 * d, lane), pf, dv[d]);
+        dk[d] = mfma32(ga_trfrag<GA_STEP>(tq, 16 * mm, 32 * d, lane), sf, dk[d]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < D / 4; i++) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+    }
+  };
+  if (steps) {
+    f32x16 s, dp, s2, dp2;
+    load(Const<0>(), 0);
+    load(Const<1>(), 1);
+    load(Const<2>(), 2);
+    wait_vmcnt<0>();
+    __syncthreads();
+    scores(Const<0>(), s, dp);
+    for (int t = 0; t < steps; t += 4) {
+      turn(Const<0>(), t, s, dp, s2, dp2);
+      if (t + 1 < steps) turn(Const<1>(), t + 1, s2, dp2, s, dp);
+      if (t + 2 < steps) turn(Const<2>(), t + 2, s, dp, s2, dp2);
+      if (t + 3 < steps) turn(Const<3>(), t + 3, s2, dp2, s, dp);
+    }
   }
   if (j0 >= a.n_k) return;
+  if (a.parts > 1) {
+    // [part][dk, dv][sequence][key][head][D]
+    const size_t rows = (size_t)a.batch * a.n_k * a.kv_heads * D;
+    float* p = a.partial + 2 * part * rows + (((size_t)it.b * a.n_k + j) * a.kv_heads + it.h) * D + 4 * half;
+    if (j < a.n_k)
+#pragma unroll
+      for (int d = 0; d < D / 32; d++)
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+          *(f32x4*)(p + 32 * d + 8 * g) = f32x4{dk[d][4 * g], dk[d][4 * g + 1], dk[d][4 * g + 2], dk[d][4 * g + 3]};
+          *(f32x4*)(p + rows + 32 * d + 8 * g) = f32x4{dv[d][4 * g], dv[d][4 * g + 1], dv[d][4 * g + 2], dv[d][4 * g + 3]};
+        }
+    return;
+  }
   bf16* dkb = a.dk + ((size_t)it.b * a.n_k + j0) * a.dk_stride + (size_t)it.h * D;
   bf16* dvb = a.dv + ((size_t)it.b * a.n_k + j0) * a.dv_stride + (size_t)it.h * D;
 #pragma unroll
@@ -388,90 +543,27 @@ __global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(
   }
 }
 
-// dQ of 128 queries of one head: over the key tiles they see, S^T and dP^T with
-// lanes = queries.
-template <int D>
-__global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_q_kernel(GroupedArgs a,
-                                                                               int total) {
-  __shared__ __attribute__((aligned(1024))) bf16 sK[2][GA_TILE * D], sV[2][GA_TILE * D];
-  Item it;
-  if (!ga_item(a.q_heads, (a.n_q + GA_ROWS - 1) / GA_ROWS, total, a.causal, &it)) return;
-  const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = wave_index<GA_THREADS / 64>();
-  const int kvh = it.h / a.group, len = ga_length(a, it.b), off = a.n_k - a.n_q;
-  const int blk0 = it.tile * GA_ROWS, q0 = blk0 + 32 * wave;
-  const int pad = (a.n_q + GA_TILE - 1) / GA_TILE * GA_TILE;
-  const bf16* qb = a.q + (size_t)it.b * a.n_q * a.q_stride + (size_t)it.h * D;
-  const size_t os = (size_t)a.q_heads * D;
-  const bf16* ob = a.dout + (size_t)it.b * a.n_q * os + (size_t)it.h * D;
-  const bf16* kb = a.k + (size_t)it.b * a.n_k * a.k_stride + (size_t)kvh * D;
-  const bf16* vb = a.v + (size_t)it.b * a.n_k * a.v_stride + (size_t)kvh * D;
-  const int blk_end = a.causal ? min(len, blk0 + GA_ROWS + off) : len;
-  const int wave_end = a.causal ? min(len, q0 + 32 + off) : len;
-  const int full_end = a.causal ? min(len, q0 + 1 + off) : len;
-  const int tiles = blk_end > 0 ? (blk_end + GA_TILE - 1) / GA_TILE : 0;
-  bf16x8 qf[D / 16], of[D / 16];
-  ga_rows<D>(qf, qb, a.q_stride, q0, a.n_q, lane);
-  ga_rows<D>(of, ob, os, q0, a.n_q, lane);
-  float lq = INFINITY, dq = 0.f;
-  if (q0 + (lane & 31) < a.n_q) {
-    const size_t row = ((size_t)it.b * a.q_heads + it.h) * pad + q0 + (lane & 31);
-    lq = a.row_lse[row];
-    dq = a.row_sum[row];
+// Adds the parts of dK (blockIdx.y 0) or dV, eight columns to a thread.
+__global__ __launch_bounds__(GA_THREADS) void ga_join_kernel(GroupedArgs a) {
+  const int width = a.kv_heads * a.head_dim;
+  const size_t i = ((size_t)blockIdx.x * GA_THREADS + threadIdx.x) * 8;
+  const size_t rows = (size_t)a.batch * a.n_k * width;
+  if (i >= rows) return;
+  const float* p = a.partial + blockIdx.y * rows + i;
+  f32x4 x = {}, y = {};
+  for (int part = 0; part < a.parts; part++, p += 2 * rows) {
+    x += *(const f32x4*)p;
+    y += *(const f32x4*)(p + 4);
   }
-  f32x16 gq[D / 32] = {};
-  const float sc = a.scale * GA_LOG2E;
-  TileLoad<D> lk, lv;
-  if (tiles) {
-    lk.load(kb, a.k_stride, 0, len);
-    lv.load(vb, a.v_stride, 0, len);
-    lk.store(sK[0]);
-    lv.store(sV[0]);
+  const float scale = blockIdx.y ? 1.f : a.scale;
+  bf16x8 v;
+#pragma unroll
+  for (int e = 0; e < 4; e++) {
+    v[e] = to_bf16(x[e] * scale);
+    v[4 + e] = to_bf16(y[e] * scale);
   }
-  for (int t = 0; t < tiles; t++) {
-    __syncthreads();
-    if (t + 1 < tiles) {
-      lk.load(kb, a.k_stride, (t + 1) * GA_TILE, len);
-      lv.load(vb, a.v_stride, (t + 1) * GA_TILE, len);
-    }
-    const bf16 *tk = sK[t & 1], *tv = sV[t & 1];
-    const int k0 = t * GA_TILE;
-#pragma unroll
-    for (int kt = 0; kt < 2; kt++) {
-      if (k0 + 32 * kt >= wave_end) continue;       // wave-uniform
-      f32x16 s = {}, dp = {};
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ks++) {
-        s = mfma32(ga_frag<D>(tk, 32 * kt, 16 * ks, lane), qf[ks], s);
-        dp = mfma32(ga_frag<D>(tv, 32 * kt, 16 * ks, lane), of[ks], dp);
-      }
-#pragma unroll
-      for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], sc, -lq));
-      if (k0 + 32 * kt + 32 > full_end) {
-        const int end = a.causal ? min(len, q0 + (lane & 31) + 1 + off) : len;
-#pragma unroll
-        for (int e = 0; e < 16; e++)
-          if (k0 + 32 * kt + 8 * (e >> 2) + 4 * half + (e & 3) >= end) s[e] = 0.f;
-      }
-#pragma unroll
-      for (int e = 0; e < 16; e++) s[e] *= dp[e] - dq;
-#pragma unroll
-      for (int mm = 0; mm < 2; mm++) {
-        const bf16x8 sf = att_pack(s, mm);
-#pragma unroll
-        for (int d = 0; d < D / 32; d++)
-          gq[d] = mfma32(ga_trfrag<D>(tk, 32 * kt + 16 * mm, 32 * d, lane), sf, gq[d]);
-      }
-    }
-    if (t + 1 < tiles) {
-      lk.store(sK[(t + 1) & 1]);
-      lv.store(sV[(t + 1) & 1]);
-    }
-  }
-  if (q0 >= a.n_q) return;
-  bf16* dqb = a.dq + ((size_t)it.b * a.n_q + q0) * a.dq_stride + (size_t)it.h * D;
-#pragma unroll
-  for (int d = 0; d < D / 32; d++) att_store(dqb + 32 * d, a.dq_stride, gq[d], a.scale, lane, a.n_q - q0);
+  const size_t row = i / width, col = i - row * width;
+  *(bf16x8*)((blockIdx.y ? a.dv + row * a.dv_stride : a.dk + row * a.dk_stride) + col) = v;
 }
 
 // Sequences [b0, b0 + nb) of a call.
@@ -486,13 +578,11 @@ GroupedArgs ga_slice(const GroupedArgs& a, int64_t b0, int64_t nb) {
   s.lse += qo * a.q_heads;
   if (a.lengths) s.lengths += b0;
   if (a.dout) {
-    const size_t pad = (size_t)(a.n_q + GA_TILE - 1) / GA_TILE * GA_TILE;
     s.dout += qo * hd;
     s.dq += qo * a.dq_stride;
     s.dk += ko * a.dk_stride;
     s.dv += ko * a.dv_stride;
-    s.row_sum += (size_t)b0 * a.q_heads * pad;
-    s.row_lse += (size_t)b0 * a.q_heads * pad;
+    s.stats += (size_t)b0 * a.q_heads * ((a.n_q + 31) / 32) * 64;
   }
   return s;
 }
@@ -515,34 +605,52 @@ hipError_t ga_forward(const GroupedArgs& a, hipStream_t st) {
   return hipSuccess;
 }
 
+// Blocks that share a key tile: as many as give the chip two blocks per CU, each
+// with four query tiles at least.
+int ga_parts(int64_t batch, int64_t n_q, int64_t n_k, int q_heads, int kv_heads) {
+  const int64_t blocks = batch * kv_heads * ga_tiles((int)n_k);
+  const int64_t steps = (n_q + GA_STEP - 1) / GA_STEP * (q_heads / kv_heads);
+  const int64_t want = 512 / blocks, most = steps / 4;
+  const int64_t p = want < most ? want : most;
+  return p < 1 ? 1 : p > 32 ? 32 : (int)p;
+}
+
+size_t ga_stats_bytes(int64_t batch, int64_t n_q, int q_heads) {
+  return (size_t)batch * q_heads * ((n_q + 31) / 32) * 64 * sizeof(float);
+}
+
 template <int D>
 hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
-  const int pad = (a.n_q + GA_TILE - 1) / GA_TILE * GA_TILE;
-  const int64_t rows = (int64_t)a.q_heads * (pad / 32), rpb = GA_THREADS / 64;
-  const int64_t kv = ga_tiles(a.n_k) * a.kv_heads, q = ga_tiles(a.n_q) * a.q_heads;
-  const int64_t per = std::max(std::max(kv, q), (rows + rpb - 1) / rpb);
+  const int64_t kv = ga_tiles(a.n_k) * a.kv_heads * a.parts, q = ga_tiles(a.n_q) * a.q_heads;
+  const int64_t per = std::max(kv, q);
+  // (parts > 1 has few blocks, hence one slice: the sums' places depend on the batch)
   const int64_t most = GA_MAX_BLOCKS / per > 0 ? GA_MAX_BLOCKS / per : 1;
   for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
     const int64_t nb = a.batch - b0 < most ? a.batch - b0 : most;
     const GroupedArgs s = ga_slice(a, b0, nb);
-    ga_row_sum_kernel<D><<<(int)((nb * rows + rpb - 1) / rpb), GA_THREADS, 0, st>>>(s, pad, (int)(nb * rows));
+    ga_bwd_q_kernel<D><<<ga_grid(nb * q), GA_THREADS, 0, st>>>(s, (int)(nb * q));
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     ga_bwd_kv_kernel<D><<<ga_grid(nb * kv), GA_THREADS, 0, st>>>(s, (int)(nb * kv));
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    ga_bwd_q_kernel<D><<<ga_grid(nb * q), GA_THREADS, 0, st>>>(s, (int)(nb * q));
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (a.parts > 1) {
+      const int64_t vecs = (int64_t)nb * a.n_k * a.kv_heads * (D / 8);
+      ga_join_kernel<<<dim3((unsigned)((vecs + GA_THREADS - 1) / GA_THREADS), 2), GA_THREADS, 0, st>>>(s);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
   }
   return hipSuccess;
 }
 
 }  // namespace
 
-size_t grouped_workspace_bytes(int64_t batch, int64_t n_q, int32_t q_heads) {
-  const size_t pad = (size_t)(n_q + GA_TILE - 1) / GA_TILE * GA_TILE;
-  return ((size_t)batch * q_heads * pad * 2 * sizeof(float) + 255) / 256 * 256;
+size_t grouped_workspace_bytes(int64_t batch, int64_t n_q, int64_t n_k, int32_t q_heads,
+                               int32_t kv_heads, int32_t head_dim) {
+  const int parts = ga_parts(batch, n_q, n_k, q_heads, kv_heads);
+  const size_t sums = parts > 1 ? (size_t)parts * 2 * batch * n_k * kv_heads * head_dim * sizeof(float) : 0;
+  return (ga_stats_bytes(batch, n_q, q_heads) + sums + 255) / 256 * 256;
 }
 
 hipError_t launch_grouped_forward(const GroupedArgs& a, hipStream_t st) {
@@ -550,9 +658,9 @@ hipError_t launch_grouped_forward(const GroupedArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_grouped_backward(GroupedArgs a, void* workspace, hipStream_t st) {
-  const size_t pad = (size_t)(a.n_q + GA_TILE - 1) / GA_TILE * GA_TILE;
-  a.row_sum = (float*)workspace;
-  a.row_lse = a.row_sum + (size_t)a.batch * a.q_heads * pad;
+  a.parts = ga_parts(a.batch, a.n_q, a.n_k, a.q_heads, a.kv_heads);
+  a.stats = (float*)workspace;
+  a.partial = a.stats + ga_stats_bytes(a.batch, a.n_q, a.q_heads) / sizeof(float);
   return a.head_dim == 64 ? ga_backward<64>(a, st) : ga_backward<128>(a, st);
 }
 
