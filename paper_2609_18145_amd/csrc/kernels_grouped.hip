@@ -74,17 +74,32 @@ struct TileDma {
   }
 };
 
-// This block's (sequence, head, tile): the tiles of one head, and the heads of
-// one group, are neighbours on one XCD, whose L2 then holds their keys and
-// values; a head's tiles with the most work come first.
+// This block's (sequence, head, tile).  Under a causal mask a head's tiles differ
+// in work up to its whole length, and a heavy one that starts late is waited for:
+// tiles come in order of their work, the heaviest of all heads first (8 x 4096,
+// 16 heads over 4: head after head, dK and dV took 870 us, so 600).  The heads are
+// dealt to the XCDs (blocks go to the 8 of them in turn), so that an L2 holds the
+// keys and values that a group's heads and a head's tiles share, and on an XCD
+// taken in chunks of two rounds of its 64 blocks.  A number of heads that is no
+// multiple of 8 is spread over the XCDs as it comes.
 struct Item {
   int b, h, tile;
 };
-__device__ __forceinline__ bool ga_item(int heads, int tiles, int total, bool last_first, Item* it) {
-  const int chunk = (total + 7) >> 3;
-  const int i = (blockIdx.x & 7) * chunk + (blockIdx.x >> 3);
-  if ((blockIdx.x >> 3) >= chunk || i >= total) return false;
-  const int bh = i / tiles, t = i - bh * tiles;
+__device__ __forceinline__ bool ga_item(int batch, int heads, int tiles, bool last_first, Item* it) {
+  const unsigned all = (unsigned)batch * heads;
+  unsigned bh, t;
+  if (blockIdx.x >= all * tiles) return false;
+  if (all % 8 == 0) {
+    const unsigned per = all / 8, xcd = blockIdx.x % 8, k = blockIdx.x / 8;
+    const unsigned two = (127u + tiles) / tiles, size = min(per, two);
+    const unsigned chunk = k / (size * tiles), r = k - chunk * size * tiles;
+    const unsigned n = min(size, per - chunk * size);
+    t = r / n;
+    bh = xcd * per + chunk * size + (r - t * n);
+  } else {
+    t = blockIdx.x / all;
+    bh = blockIdx.x - t * all;
+  }
   it->b = bh / heads;
   it->h = bh - it->b * heads;
   it->tile = last_first ? tiles - 1 - t : t;
@@ -127,10 +142,10 @@ __device__ __forceinline__ void ga_rows(bf16x8 (&f)[D / 16], const bf16* base, s
 constexpr float GA_SLACK = 8.f;
 
 template <int D>
-__global__ __launch_bounds__(GA_THREADS, 2) void ga_fwd_kernel(GroupedArgs a, int total) {
+__global__ __launch_bounds__(GA_THREADS, 2) void ga_fwd_kernel(GroupedArgs a) {
   __shared__ __attribute__((aligned(1024))) bf16 sK[2][GA_TILE * D], sV[2][GA_TILE * D];
   Item it;
-  if (!ga_item(a.q_heads, (a.n_q + GA_ROWS - 1) / GA_ROWS, total, a.causal, &it)) return;
+  if (!ga_item(a.batch, a.q_heads, (a.n_q + GA_ROWS - 1) / GA_ROWS, a.causal, &it)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = wave_index<GA_THREADS / 64>();
   const int kvh = it.h / a.group, len = ga_length(a, it.b), off = a.n_k - a.n_q;
@@ -271,10 +286,10 @@ __device__ __forceinline__ size_t ga_stats(int bh, int n_q, int row0) {
 }
 
 template <int D>
-__global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a, int total) {
+__global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) {
   __shared__ __attribute__((aligned(1024))) bf16 sK[GA_BUFS][GA_STEP * D], sV[GA_BUFS][GA_STEP * D];
   Item it;
-  if (!ga_item(a.q_heads, (a.n_q + GA_ROWS - 1) / GA_ROWS, total, a.causal, &it)) return;
+  if (!ga_item(a.batch, a.q_heads, (a.n_q + GA_ROWS - 1) / GA_ROWS, a.causal, &it)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = wave_index<GA_THREADS / 64>();
   const int kvh = it.h / a.group, len = ga_length(a, it.b), off = a.n_k - a.n_q;
@@ -377,11 +392,6 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a, 
       for (int dt = 0; dt < D / 32; dt++)
         gq[dt] = mfma32(ga_trfrag<GA_STEP>(tk, 16 * mm, 32 * dt, lane), sf, gq[dt]);
     }
-#pragma unroll
-    for (int i = 0; i < 3 * D / 16; i++) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
-    }
   };
   if (tiles) {
     f32x16 s, dp, s2, dp2;
@@ -407,15 +417,14 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a, 
 // the key tiles are too few for the chip, a.parts blocks share that sequence of
 // query tiles and leave fp32 sums, which ga_join_kernel adds in order.
 template <int D>
-__global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(GroupedArgs a,
-                                                                                int total) {
+__global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(GroupedArgs a) {
   __shared__ __attribute__((aligned(1024))) bf16 sQ[GA_BUFS][GA_STEP * D], sO[GA_BUFS][GA_STEP * D];
   // a tile's statistics, four times over: every wave copies them, to keep one
   // count of loads on their way, and 64 lanes copy 1 KB
   __shared__ __attribute__((aligned(1024))) float sS[GA_BUFS][256];
   Item it;
   const int key_tiles = (a.n_k + GA_ROWS - 1) / GA_ROWS;
-  if (!ga_item(a.kv_heads, key_tiles * a.parts, total, false, &it)) return;
+  if (!ga_item(a.batch, a.kv_heads, key_tiles * a.parts, false, &it)) return;
   const int part = it.tile % a.parts;
   it.tile /= a.parts;
   const int lane = threadIdx.x & 63, half = lane >> 5;
@@ -497,11 +506,6 @@ __global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(
         dv[d] = mfma32(ga_trfrag<GA_STEP>(to, 16 * mm, 32 * d, lane), pf, dv[d]);
         dk[d] = mfma32(ga_trfrag<GA_STEP>(tq, 16 * mm, 32 * d, lane), sf, dk[d]);
       }
-    }
-#pragma unroll
-    for (int i = 0; i < D / 4; i++) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
     }
   };
   if (steps) {
@@ -587,9 +591,7 @@ GroupedArgs ga_slice(const GroupedArgs& a, int64_t b0, int64_t nb) {
   return s;
 }
 
-// A launch's blocks: below 2^32 threads, and whole rounds of the 8 XCDs.
-constexpr int64_t GA_MAX_BLOCKS = 1 << 23;
-int ga_grid(int64_t total) { return (int)((total + 7) / 8 * 8); }
+constexpr int64_t GA_MAX_BLOCKS = 1 << 23;     // of a launch: below 2^32 threads
 int64_t ga_tiles(int n) { return (n + GA_ROWS - 1) / GA_ROWS; }
 
 template <int D>
@@ -597,8 +599,8 @@ hipError_t ga_forward(const GroupedArgs& a, hipStream_t st) {
   const int64_t per = ga_tiles(a.n_q) * a.q_heads;
   const int64_t most = GA_MAX_BLOCKS / per > 0 ? GA_MAX_BLOCKS / per : 1;
   for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
-    const int64_t nb = a.batch - b0 < most ? a.batch - b0 : most, total = nb * per;
-    ga_fwd_kernel<D><<<ga_grid(total), GA_THREADS, 0, st>>>(ga_slice(a, b0, nb), (int)total);
+    const int64_t nb = a.batch - b0 < most ? a.batch - b0 : most;
+    ga_fwd_kernel<D><<<(int)(nb * per), GA_THREADS, 0, st>>>(ga_slice(a, b0, nb));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -628,10 +630,10 @@ hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
   for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
     const int64_t nb = a.batch - b0 < most ? a.batch - b0 : most;
     const GroupedArgs s = ga_slice(a, b0, nb);
-    ga_bwd_q_kernel<D><<<ga_grid(nb * q), GA_THREADS, 0, st>>>(s, (int)(nb * q));
+    ga_bwd_q_kernel<D><<<(int)(nb * q), GA_THREADS, 0, st>>>(s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    ga_bwd_kv_kernel<D><<<ga_grid(nb * kv), GA_THREADS, 0, st>>>(s, (int)(nb * kv));
+    ga_bwd_kv_kernel<D><<<(int)(nb * kv), GA_THREADS, 0, st>>>(s);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (a.parts > 1) {
