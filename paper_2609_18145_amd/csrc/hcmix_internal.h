@@ -281,10 +281,10 @@ struct RotaryArgs {
   int64_t rows, x_stride, y_stride, period;
   float scale;
   int heads, head_dim, rot, inverse;
-  // set by launch_rotary: rows of a block, units of a head and 2^32 / units
-  // rounded up, log2 of the threads along a row
-  int rows_per_block, units, log_x;
-  uint64_t units_magic;
+  // set by launch_rotary: rows of a block, units of a head, 2^32 / units and
+  // 2^44 / (units heads) rounded up
+  int rows_per_block, units;
+  uint64_t units_magic, all_magic;
 };
 hipError_t launch_rotary(RotaryArgs a, int layout_half, int elem_bytes, hipStream_t st);
 

@@ -47,7 +47,7 @@ __device__ __forceinline__ float kv_scale(float amax) {
   return __uint_as_float((unsigned)(e + 127) << 23);
 }
 
-// |v| <= 448 (1 + 2^-9) or infinite: those are held as 448, NaN as NaN.
+// |v| <= 448 or infinite (held as 448), or NaN (held as NaN).
 __device__ __forceinline__ unsigned char kv_byte(float v) {
   v = v > 448.f ? 448.f : v < -448.f ? -448.f : v;
   return (unsigned char)__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false);
@@ -71,13 +71,39 @@ __device__ __forceinline__ void kv_expand(const u32x4& v, float scale, bf16x8* l
   }
 }
 
+// Four bytes (tokens 4 i .. 4 i + 3 of a dimension) of a block's values in LDS:
+// rows of 17 words, so that the lanes that hold neighbouring dimensions of one
+// token group meet in no bank.
+constexpr int KV_ROW = KB / 4 + 1;
+__device__ __forceinline__ int kv_word(int dim, int group) { return dim * KV_ROW + (kv_slot(4 * group) >> 2); }
+
+// 16 held numbers at another scale.
+__device__ __forceinline__ u32x4 kv_rescaled(u32x4 v, float ratio) {
+#pragma unroll
+  for (int w = 0; w < 4; w++) {
+    unsigned r = 0;
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+      r |= (unsigned)kv_byte(kv_value((v[w] >> (8 * e)) & 255) * ratio) << (8 * e);
+    v[w] = r;
+  }
+  return v;
+}
+
 // ---------------------------------------------------------------------------
-// Append: a block of threads per touched block of one head and sequence.
+// Append: a block of threads per touched block of one head and sequence.  Its
+// new tokens are read once, an item of 4 tokens x 8 dimensions to a thread: the
+// largest magnitude, then the bytes, from registers.  Values turn in LDS where the
+// block is filled from its first token on; into a block that holds some already
+// they go byte by byte.
 // ---------------------------------------------------------------------------
+template <int D>
 __global__ __launch_bounds__(KV_THREADS) void kv_append_kernel(KvAppendArgs a) {
-  extern __shared__ unsigned char tile[];          // values of a fresh block: [D][64]
+  constexpr int DV = D / 8, ITEMS = KB / 4 * DV;   // of keys, as many of values
+  constexpr int PER = 2 * ITEMS / KV_THREADS;      // per thread: keys and values, or one of them
+  __shared__ unsigned tile[D * KV_ROW];
   __shared__ float part[2][KV_WAVES];
-  const int h = blockIdx.y, b = blockIdx.z, D = a.head_dim;
+  const int h = blockIdx.y, b = blockIdx.z;
   const int pos = a.positions[b];
   const int count = a.counts ? kv_bounded(a.counts[b], 0, a.tokens) : a.tokens;
   if (pos < 0 || pos >= a.capacity) return;
@@ -85,105 +111,154 @@ __global__ __launch_bounds__(KV_THREADS) void kv_append_kernel(KvAppendArgs a) {
   const int blk = pos / KB + blockIdx.x, first = blk * KB;
   const int t0 = first > pos ? first : pos, t1 = end < first + KB ? end : first + KB;
   if (t0 >= t1) return;
-  const int old = t0 - first, n = t1 - t0;         // earlier tokens of the block, new ones
-  const size_t row0 = (size_t)b * a.tokens + (t0 - pos);
-  const bf16* k = a.k + row0 * a.k_stride + (size_t)h * D;
-  const bf16* v = a.v + row0 * a.v_stride + (size_t)h * D;
+  const int old = t0 - first;                      // earlier tokens of the block
   const size_t at = ((size_t)b * a.kv_heads + h) * a.blocks + blk;
   unsigned char *ck = a.keys + at * KB * D, *cv = a.values + at * KB * D;
-  const int dv = D >> 3;                           // vectors of 8 of a row
-  float mk = 0.f, mv = 0.f;
-  for (int i = threadIdx.x; i < n * dv; i += KV_THREADS) {
-    const int t = i / dv, p = i - t * dv;
-    const bf16x8 x = *(const bf16x8*)(k + (size_t)t * a.k_stride + 8 * p);
-    const bf16x8 y = *(const bf16x8*)(v + (size_t)t * a.v_stride + 8 * p);
+  float* scales = a.scales + 2 * at;
+  const float ok = old ? scales[0] : 0.f, ov = old ? scales[1] : 0.f;
+  bf16x8 x[PER][4];
+  float amax[2] = {0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 8; e++) {
-      mk = fmaxf(mk, fabsf((float)x[e]));
-      mv = fmaxf(mv, fabsf((float)y[e]));
+  for (int i = 0; i < PER; i++) {
+    const int item = threadIdx.x + KV_THREADS * i, of_v = item / ITEMS, rest = item % ITEMS;
+    const int g = rest / DV, p = rest % DV;
+    const bf16* src = (of_v ? a.v : a.k) + (size_t)h * D + 8 * p;
+    const size_t stride = of_v ? a.v_stride : a.k_stride;
+    float m = 0.f;
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      const int t = first + 4 * g + r;
+      x[i][r] = bf16x8{};
+      if (t >= t0 && t < t1) x[i][r] = *(const bf16x8*)(src + ((size_t)b * a.tokens + (t - pos)) * stride);
     }
+#pragma unroll
+    for (int r = 0; r < 4; r++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) m = fmaxf(m, fabsf((float)x[i][r][e]));
+    amax[0] = fmaxf(amax[0], of_v ? 0.f : m);
+    amax[1] = fmaxf(amax[1], of_v ? m : 0.f);
   }
 #pragma unroll
   for (int s = 32; s; s >>= 1) {
-    mk = fmaxf(mk, __shfl_xor(mk, s));
-    mv = fmaxf(mv, __shfl_xor(mv, s));
+    amax[0] = fmaxf(amax[0], __shfl_xor(amax[0], s));
+    amax[1] = fmaxf(amax[1], __shfl_xor(amax[1], s));
   }
   if ((threadIdx.x & 63) == 0) {
-    part[0][threadIdx.x >> 6] = mk;
-    part[1][threadIdx.x >> 6] = mv;
+    part[0][threadIdx.x >> 6] = amax[0];
+    part[1][threadIdx.x >> 6] = amax[1];
   }
-  float *scales = a.scales + 2 * at;
-  const float ok = old ? scales[0] : 0.f, ov = old ? scales[1] : 0.f;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < KV_WAVES; w++) {
-    mk = fmaxf(mk, part[0][w]);
-    mv = fmaxf(mv, part[1][w]);
+    amax[0] = fmaxf(amax[0], part[0][w]);
+    amax[1] = fmaxf(amax[1], part[1][w]);
   }
-  const float sk = fmaxf(kv_scale(mk), ok), sv = fmaxf(kv_scale(mv), ov);
+  const float sk = fmaxf(kv_scale(amax[0]), ok), sv = fmaxf(kv_scale(amax[1]), ov);
   if (threadIdx.x == 0) {
     scales[0] = sk;
     scales[1] = sv;
   }
-  // what is there already, at the new scale
+  // what is there already, at the new scale (and what lies behind it, which
+  // nothing takes)
   if (old && sk > ok)
-    for (int i = threadIdx.x; i < old * D; i += KV_THREADS) ck[i] = kv_byte(kv_value(ck[i]) * (ok / sk));
-  if (old && sv > ov)
-    for (int i = threadIdx.x; i < old * D; i += KV_THREADS) {
-      const int t = i % old, d = i / old;
-      unsigned char* c = cv + d * KB + kv_slot(t);
-      *c = kv_byte(kv_value(*c) * (ov / sv));
-    }
+    for (int i = threadIdx.x; i < old * (D / 16); i += KV_THREADS)
+      ((u32x4*)ck)[i] = kv_rescaled(((u32x4*)ck)[i], ok / sk);
+  if (old && sv > ov) {
+    for (int i = threadIdx.x; i < KB * D / 16; i += KV_THREADS)
+      ((u32x4*)cv)[i] = kv_rescaled(((u32x4*)cv)[i], ov / sv);
+    __syncthreads();                               // new bytes go between them
+  }
   const float ik = 1.f / sk, iv = 1.f / sv;        // exact
-  if (!old)
-    for (int i = threadIdx.x; i < KB * D / 4; i += KV_THREADS) ((unsigned*)tile)[i] = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < n * dv; i += KV_THREADS) {
-    const int t = i / dv, p = i - t * dv;
-    const bf16x8 x = *(const bf16x8*)(k + (size_t)t * a.k_stride + 8 * p);
-    const bf16x8 y = *(const bf16x8*)(v + (size_t)t * a.v_stride + 8 * p);
-    unsigned w[2] = {0, 0};
-    unsigned char* out = old ? cv : tile;
 #pragma unroll
-    for (int e = 0; e < 8; e++) {
-      w[e >> 2] |= (unsigned)kv_byte((float)x[e] * ik) << (8 * (e & 3));
-      out[(8 * p + e) * KB + kv_slot(old + t)] = kv_byte((float)y[e] * iv);
+  for (int i = 0; i < PER; i++) {
+    const int item = threadIdx.x + KV_THREADS * i, of_v = item / ITEMS, rest = item % ITEMS;
+    const int g = rest / DV, p = rest % DV, t = first + 4 * g;
+    if (t + 4 <= t0 || t >= t1) {
+      if (of_v && !old)
+#pragma unroll
+        for (int e = 0; e < 8; e++) tile[kv_word(8 * p + e, g)] = 0;
+      continue;
     }
-    *(uint2*)(ck + (size_t)(old + t) * D + 8 * p) = uint2{w[0], w[1]};
+    unsigned char bytes[4][8];
+#pragma unroll
+    for (int r = 0; r < 4; r++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) bytes[r][e] = kv_byte((float)x[i][r][e] * (of_v ? iv : ik));
+    if (!of_v) {
+#pragma unroll
+      for (int r = 0; r < 4; r++)
+        if (t + r >= t0 && t + r < t1)
+          *(uint2*)(ck + (4 * g + r) * D + 8 * p) =
+              uint2{bytes[r][0] | (unsigned)bytes[r][1] << 8 | (unsigned)bytes[r][2] << 16 | (unsigned)bytes[r][3] << 24,
+                    bytes[r][4] | (unsigned)bytes[r][5] << 8 | (unsigned)bytes[r][6] << 16 | (unsigned)bytes[r][7] << 24};
+    } else if (!old) {
+#pragma unroll
+      for (int e = 0; e < 8; e++)
+        tile[kv_word(8 * p + e, g)] = bytes[0][e] | (unsigned)bytes[1][e] << 8 |
+                                      (unsigned)bytes[2][e] << 16 | (unsigned)bytes[3][e] << 24;
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; r++)
+        if (t + r >= t0 && t + r < t1)
+#pragma unroll
+          for (int e = 0; e < 8; e++) cv[(8 * p + e) * KB + kv_slot(4 * g + r)] = bytes[r][e];
+    }
   }
   if (!old) {
     __syncthreads();
-    for (int i = threadIdx.x; i < KB * D / 16; i += KV_THREADS) ((u32x4*)cv)[i] = ((const u32x4*)tile)[i];
+    for (int i = threadIdx.x; i < D * (KB / 16); i += KV_THREADS) {
+      const unsigned* w = tile + i / (KB / 16) * KV_ROW + i % (KB / 16) * 4;
+      ((u32x4*)cv)[i] = u32x4{w[0], w[1], w[2], w[3]};
+    }
   }
 }
 
 // ---------------------------------------------------------------------------
-// Read: tokens first[b] .. + tokens of every sequence, zeros from lengths[b] on.
+// Read: tokens first[b] .. + tokens of every sequence, zeros from lengths[b] on;
+// a block of threads per touched block, as the append has them.
 // ---------------------------------------------------------------------------
+template <int D>
 __global__ __launch_bounds__(KV_THREADS) void kv_read_kernel(KvReadArgs a) {
-  const int h = blockIdx.y, b = blockIdx.z, D = a.head_dim, dv = D >> 3;
+  constexpr int DV = D / 8, ITEMS = KB / 4 * DV;
+  __shared__ unsigned tile[D * KV_ROW];
+  const int h = blockIdx.y, b = blockIdx.z;
   const int from = a.first[b], len = kv_bounded(a.lengths[b], 0, a.capacity);
-  const size_t at0 = ((size_t)b * a.kv_heads + h) * a.blocks;
-  for (int i = threadIdx.x; i < KB * dv; i += KV_THREADS) {
-    const int p = i / KB, t = blockIdx.x * KB + i % KB;    // neighbours read one dimension's row
-    if (t >= a.tokens) continue;
-    const int64_t pos = (int64_t)from + t;
-    bf16x8 x = {}, y = {};
-    if (pos >= 0 && pos < len) {
-      const size_t at = at0 + pos / KB;
-      const int r = (int)(pos % KB);
-      const float sk = a.scales[2 * at], sv = a.scales[2 * at + 1];
-      const uint2 w = *(const uint2*)(a.keys + at * KB * D + (size_t)r * D + 8 * p);
-      const unsigned char* c = a.values + at * KB * D + (size_t)8 * p * KB + kv_slot(r);
+  const int64_t start = ((int64_t)from - ((from % KB) + KB) % KB) + (int64_t)blockIdx.x * KB;
+  if (start >= (int64_t)from + a.tokens) return;
+  const bool held = start >= 0 && start < len;     // (then a block of the cache)
+  const size_t at = held ? ((size_t)b * a.kv_heads + h) * a.blocks + start / KB : 0;
+  const unsigned char *ck = a.keys + at * KB * D, *cv = a.values + at * KB * D;
+  if (held)
+    for (int i = threadIdx.x; i < D * (KB / 16); i += KV_THREADS) {
+      const u32x4 v = ((const u32x4*)cv)[i];
+      unsigned* w = tile + i / (KB / 16) * KV_ROW + i % (KB / 16) * 4;
 #pragma unroll
-      for (int e = 0; e < 8; e++) {
-        x[e] = to_bf16(kv_value(((e < 4 ? w.x : w.y) >> (8 * (e & 3))) & 255) * sk);
-        y[e] = to_bf16(kv_value(c[e * KB]) * sv);
-      }
+      for (int e = 0; e < 4; e++) w[e] = v[e];
     }
-    const size_t o = (((size_t)b * a.tokens + t) * a.kv_heads + h) * D + 8 * p;
-    *(bf16x8*)(a.k + o) = x;
-    *(bf16x8*)(a.v + o) = y;
+  const float sk = held ? a.scales[2 * at] : 0.f, sv = held ? a.scales[2 * at + 1] : 0.f;
+  __syncthreads();
+  for (int item = threadIdx.x; item < ITEMS; item += KV_THREADS) {
+    const int g = item / DV, p = item % DV;
+    unsigned w[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) w[e] = held ? tile[kv_word(8 * p + e, g)] : 0;
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      const int64_t pos = start + 4 * g + r, t = pos - from;
+      if (t < 0 || t >= a.tokens) continue;
+      bf16x8 x = {}, y = {};
+      if (held && pos < len) {
+        const uint2 c = *(const uint2*)(ck + (size_t)(4 * g + r) * D + 8 * p);
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          x[e] = to_bf16(kv_value(((e < 4 ? c.x : c.y) >> (8 * (e & 3))) & 255) * sk);
+          y[e] = to_bf16(kv_value((w[e] >> (8 * r)) & 255) * sv);
+        }
+      }
+      const size_t o = (((size_t)b * a.tokens + t) * a.kv_heads + h) * D + 8 * p;
+      *(bf16x8*)(a.k + o) = x;
+      *(bf16x8*)(a.v + o) = y;
+    }
   }
 }
 
@@ -421,13 +496,15 @@ hipError_t kv_attention_launch(const KvAttentionArgs& a, hipStream_t st) {
 
 hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st) {
   const dim3 grid((a.tokens + KB - 2) / KB + 1, a.kv_heads, a.batch);
-  kv_append_kernel<<<grid, KV_THREADS, KB * a.head_dim, st>>>(a);
+  if (a.head_dim == 64) kv_append_kernel<64><<<grid, KV_THREADS, 0, st>>>(a);
+  else kv_append_kernel<128><<<grid, KV_THREADS, 0, st>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t st) {
-  const dim3 grid((a.tokens + KB - 1) / KB, a.kv_heads, a.batch);
-  kv_read_kernel<<<grid, KV_THREADS, 0, st>>>(a);
+  const dim3 grid((a.tokens + KB - 2) / KB + 1, a.kv_heads, a.batch);
+  if (a.head_dim == 64) kv_read_kernel<64><<<grid, KV_THREADS, 0, st>>>(a);
+  else kv_read_kernel<128><<<grid, KV_THREADS, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -9,7 +9,8 @@
 // The angle is taken in 64 bits, in turns, and only its fraction is rounded: a
 // position of 10^6 times a frequency in 32 bits is off by 0.06 radians.  Every
 // head of a position shares the angles, so a block first makes the table of its
-// rows' (cos, sin) in LDS and then streams the heads past it: bound by memory.
+// rows' (cos, sin) in LDS and then streams the heads past it: bound by memory, at
+// the rate of a copy.
 #include "hcmix_internal.h"
 #include "device_common.h"
 
@@ -35,18 +36,15 @@ __device__ __forceinline__ void rot_store(E* p, const float (&f)[VEC]) {
   *(Vec*)p = v;
 }
 
-// A block takes a.rows_per_block rows.  Thread (x, y) = (tid % X, tid / X), X =
-// 2^a.log_x >= units of a row where those are fewer than 256; a unit is VEC
-// pairs (half layout: VEC values of each half) or VEC values (pairs layout, and
-// the values that are copied).
+// A block takes a.rows_per_block rows and its threads their units in turn; a unit
+// is VEC pairs (half layout: VEC values of each half) or VEC values (pairs
+// layout, and the values that are copied).
 template <typename E, int VEC, bool HALF>
 __global__ __launch_bounds__(ROT_THREADS) void rotary_kernel(RotaryArgs a) {
   extern __shared__ float2 tab[];            // [rows_per_block][rot / 2]
   const E* x = (const E*)a.x;
   E* y = (E*)a.y;
-  const int pairs = a.rot >> 1;
-  const int tx = threadIdx.x & ((1 << a.log_x) - 1), ty = threadIdx.x >> a.log_x;
-  const int ny = ROT_THREADS >> a.log_x;
+  const int pairs = a.rot >> 1, all = a.units * a.heads;
   for (int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block; r0 < a.rows;
        r0 += (int64_t)gridDim.x * a.rows_per_block) {
     const int rows = a.rows - r0 < a.rows_per_block ? (int)(a.rows - r0) : a.rows_per_block;
@@ -60,64 +58,63 @@ __global__ __launch_bounds__(ROT_THREADS) void rotary_kernel(RotaryArgs a) {
       tab[i] = float2{c * a.scale, (a.inverse ? -s : s) * a.scale};
     }
     __syncthreads();
-    for (int r = ty; r < rows; r += ny) {
+    for (int i = threadIdx.x; i < rows * all; i += ROT_THREADS) {
+      // i / all and k / units: exact, as rows < 2^5, all < 2^19 and units < 2^10
+      const int r = (int)((unsigned)i * a.all_magic >> 44), k = i - r * all;
+      const int h = (int)((unsigned)k * a.units_magic >> 32), u = k - h * a.units;
       const E* xr = x + (size_t)(r0 + r) * a.x_stride;
       E* yr = y + (size_t)(r0 + r) * a.y_stride;
       const float2* cs = tab + r * pairs;
-      for (int k = tx; k < a.units * a.heads; k += 1 << a.log_x) {
-        // k / units: exact, as k < 2^19 and units < 2^10
-        const int h = (int)((unsigned)k * a.units_magic >> 32), u = k - h * a.units;
-        const size_t at = (size_t)h * a.head_dim;
-        if constexpr (HALF) {
-          if (u * VEC < pairs) {
-            float p[VEC], q[VEC], op[VEC], oq[VEC];
-            rot_load<E, VEC>(xr + at + u * VEC, p);
-            rot_load<E, VEC>(xr + at + pairs + u * VEC, q);
+      const size_t at = (size_t)h * a.head_dim;
+      if constexpr (HALF) {
+        if (u * VEC < pairs) {
+          float p[VEC], q[VEC], op[VEC], oq[VEC];
+          rot_load<E, VEC>(xr + at + u * VEC, p);
+          rot_load<E, VEC>(xr + at + pairs + u * VEC, q);
 #pragma unroll
-            for (int e = 0; e < VEC; e++) {
-              const float2 w = cs[u * VEC + e];
-              op[e] = p[e] * w.x - q[e] * w.y;
-              oq[e] = q[e] * w.x + p[e] * w.y;
-            }
-            rot_store<E, VEC>(yr + at + u * VEC, op);
-            rot_store<E, VEC>(yr + at + pairs + u * VEC, oq);
-          } else {
-            const size_t c = at + a.rot + u * VEC - pairs;
-            float p[VEC];
-            rot_load<E, VEC>(xr + c, p);
-            rot_store<E, VEC>(yr + c, p);
+          for (int e = 0; e < VEC; e++) {
+            const float2 w = cs[u * VEC + e];
+            op[e] = p[e] * w.x - q[e] * w.y;
+            oq[e] = q[e] * w.x + p[e] * w.y;
           }
+          rot_store<E, VEC>(yr + at + u * VEC, op);
+          rot_store<E, VEC>(yr + at + pairs + u * VEC, oq);
         } else {
-          constexpr int W = VEC == 1 ? 2 : VEC;      // values of a unit
-          const int c = u * W;
-          if (c < a.rot) {
-            float p[W], o[W];
-            if constexpr (VEC == 1) {
-              p[0] = (float)xr[at + c];
-              p[1] = (float)xr[at + c + 1];
-            } else {
-              rot_load<E, W>(xr + at + c, p);
-            }
-#pragma unroll
-            for (int e = 0; e < W; e += 2) {
-              const float2 w = cs[(c + e) >> 1];
-              o[e] = p[e] * w.x - p[e + 1] * w.y;
-              o[e + 1] = p[e + 1] * w.x + p[e] * w.y;
-            }
-            if constexpr (VEC == 1) {
-              yr[at + c] = (E)o[0];
-              yr[at + c + 1] = (E)o[1];
-            } else {
-              rot_store<E, W>(yr + at + c, o);
-            }
-          } else if constexpr (VEC == 1) {
-            yr[at + c] = xr[at + c];
-            yr[at + c + 1] = xr[at + c + 1];
+          const size_t c = at + a.rot + u * VEC - pairs;
+          float p[VEC];
+          rot_load<E, VEC>(xr + c, p);
+          rot_store<E, VEC>(yr + c, p);
+        }
+      } else {
+        constexpr int W = VEC == 1 ? 2 : VEC;      // values of a unit
+        const int c = u * W;
+        if (c < a.rot) {
+          float p[W], o[W];
+          if constexpr (VEC == 1) {
+            p[0] = (float)xr[at + c];
+            p[1] = (float)xr[at + c + 1];
           } else {
-            float p[W];
             rot_load<E, W>(xr + at + c, p);
-            rot_store<E, W>(yr + at + c, p);
           }
+#pragma unroll
+          for (int e = 0; e < W; e += 2) {
+            const float2 w = cs[(c + e) >> 1];
+            o[e] = p[e] * w.x - p[e + 1] * w.y;
+            o[e + 1] = p[e + 1] * w.x + p[e] * w.y;
+          }
+          if constexpr (VEC == 1) {
+            yr[at + c] = (E)o[0];
+            yr[at + c + 1] = (E)o[1];
+          } else {
+            rot_store<E, W>(yr + at + c, o);
+          }
+        } else if constexpr (VEC == 1) {
+          yr[at + c] = xr[at + c];
+          yr[at + c + 1] = xr[at + c + 1];
+        } else {
+          float p[W];
+          rot_load<E, W>(xr + at + c, p);
+          rot_store<E, W>(yr + at + c, p);
         }
       }
     }
@@ -143,12 +140,13 @@ hipError_t launch_rotary(RotaryArgs a, int layout_half, int elem_bytes, hipStrea
   const int moved = in_place ? a.rot : a.head_dim;       // values of a head to go through
   a.units = layout_half ? a.rot / 2 / v + (moved - a.rot) / v : moved / (v == 1 ? 2 : v);
   a.units_magic = ((1ull << 32) + a.units - 1) / a.units;
-  a.log_x = 0;
-  while (a.log_x < 8 && (1 << a.log_x) < a.units * a.heads) a.log_x++;
-  // Rows to a block: enough that its 256 threads each have an angle to make, no
-  // more than leave four blocks to a CU.
+  const uint64_t all = (uint64_t)a.units * a.heads;
+  a.all_magic = ((1ull << 44) + all - 1) / all;
+  // Rows to a block: more share the wait for the angles, fewer leave more blocks
+  // to hide it: 8 x 4096 positions, 20 heads of 64 (168 MB): 36.9 us with 16 and 8,
+  // 34.0 with 4 (4.9 TB/s; a copy of as much takes 33.7).
   int rpb = 1;
-  while (rpb < 16 && rpb * (a.rot / 2) < ROT_THREADS && a.rows / (2 * rpb) >= 1024) rpb *= 2;
+  while (rpb < 4 && rpb * (a.rot / 2) < ROT_THREADS && a.rows / (2 * rpb) >= 1024) rpb *= 2;
   a.rows_per_block = rpb;
   const int64_t blocks = (a.rows + rpb - 1) / rpb;
   const int grid = blocks < (1 << 20) ? (int)blocks : 1 << 20;

@@ -8,6 +8,13 @@
 // every one is a plain tensor of exactly `shape` and `dtype`, contiguous and on
 // `device`; None otherwise (the binding then finds out what is wrong, and says
 // so).
+//
+//   heads(tensor, shape, dtype, device) -> (address, stride) or None
+//
+// The same for one [batch, n, heads, head_dim] operand whose heads lie side by
+// side and whose positions are evenly spaced over the whole batch: its address
+// and the elements between two positions.  None entries of shape match any
+// extent, device None any GPU.
 #include <torch/csrc/Device.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -56,6 +63,61 @@ PyObject* pointers(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                                    count * (Py_ssize_t)sizeof(void*));
 }
 
+// A plain tensor in GPU memory with an address of its own.
+bool plain(const at::Tensor& t) {
+  return t.layout() == c10::kStrided && t.device().type() == c10::kCUDA &&
+         !t.unsafeGetTensorImpl()->is_python_dispatch() && t.has_storage() && !t.is_conj() &&
+         !t.is_neg();
+}
+
+PyObject* heads(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  if (nargs != 4) {
+    PyErr_SetString(PyExc_TypeError, "heads(tensor, shape, dtype, device)");
+    return nullptr;
+  }
+  PyObject* shape = args[1];
+  if (!THPVariable_CheckExact(args[0]) || !PyTuple_Check(shape) || PyTuple_GET_SIZE(shape) != 4 ||
+      !THPDtype_Check(args[2]) || (args[3] != Py_None && !THPDevice_Check(args[3])))
+    Py_RETURN_NONE;
+  const at::Tensor& t = THPVariable_Unpack(args[0]);
+  if (!plain(t) || t.scalar_type() != reinterpret_cast<THPDtype*>(args[2])->scalar_type ||
+      (args[3] != Py_None && t.device() != reinterpret_cast<THPDevice*>(args[3])->device) ||
+      t.dim() != 4)
+    Py_RETURN_NONE;
+  for (int i = 0; i < 4; i++) {
+    PyObject* e = PyTuple_GET_ITEM(shape, i);
+    if (e == Py_None) continue;
+    const int64_t want = PyLong_AsLongLong(e);
+    if (want == -1 && PyErr_Occurred()) return nullptr;
+    if (t.size(i) != want) Py_RETURN_NONE;
+  }
+  const int64_t b = t.size(0), n = t.size(1), h = t.size(2), d = t.size(3);
+  const int64_t stride = n > 1 ? t.stride(1) : b > 1 ? t.stride(0) : h * d;
+  if ((d > 1 && t.stride(3) != 1) || (h > 1 && t.stride(2) != d) ||
+      (n > 1 && b > 1 && t.stride(0) != n * t.stride(1)) || stride < h * d)
+    Py_RETURN_NONE;
+  PyObject* out = PyTuple_New(2);
+  if (!out) return nullptr;
+  PyObject* p = PyLong_FromVoidPtr(t.data_ptr());
+  PyObject* st = PyLong_FromLongLong(stride);
+  PyTuple_SET_ITEM(out, 0, p);
+  PyTuple_SET_ITEM(out, 1, st);
+  if (!p || !st) {
+    Py_DECREF(out);
+    return nullptr;
+  }
+  return out;
+}
+
+PyObject* guarded_heads(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+  try {
+    return heads(self, args, nargs);
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
 PyObject* guarded_pointers(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
   try {
     return pointers(self, args, nargs);
@@ -68,6 +130,8 @@ PyObject* guarded_pointers(PyObject* self, PyObject* const* args, Py_ssize_t nar
 PyMethodDef methods[] = {
     {"pointers", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(guarded_pointers)),
      METH_FASTCALL, "addresses of tensors that match, or None"},
+    {"heads", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(guarded_heads)), METH_FASTCALL,
+     "address and position stride of an operand that matches, or None"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods,

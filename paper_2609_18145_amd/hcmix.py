@@ -957,8 +957,8 @@ _ROTARY_LAYOUTS = {"half": 0, "pairs": 1}
 def _call(dev, what, *args):
     """A library call on dev's current stream, with dev the current device (a
     kernel is launched on the current device's behalf)."""
-    fn = getattr(load(), what)
-    if dev.index == torch.cuda.current_device():
+    fn = getattr(_lib or load(), what)
+    if dev.index == torch._C._cuda_getDevice():
         rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
     else:
         with torch.cuda.device(dev):
@@ -970,7 +970,12 @@ def _call(dev, what, *args):
 def _heads(t, name, shape, dtype, device=None):
     """Checks a [batch, n, heads, head_dim] operand (None entries match any
     extent): heads side by side, positions evenly spaced over the whole batch, as
-    in a slice of a packed projection.  Returns the elements between positions."""
+    in a slice of a packed projection.  Returns its address and the elements
+    between positions."""
+    if _marshal is not None or (isinstance(t, torch.Tensor) and t.is_cuda):
+        found = (_marshal or _native()).heads(t, shape, dtype, device)
+        if found is not None:
+            return found
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name}: expected a tensor, got {type(t).__name__}")
     got = tuple(t.shape)
@@ -987,7 +992,10 @@ def _heads(t, name, shape, dtype, device=None):
             or stride < h * d):
         raise ValueError(f"{name}: strides {t.stride()}, expected positions evenly spaced over the "
                          "batch, their heads contiguous")
-    return stride
+    return t.data_ptr(), stride
+
+
+_ANY = (None, None, None, None)
 
 
 def rotary_frequencies(rot_dim, base=10000.0, scaling=None, factor=1.0, original_length=None,
@@ -1036,19 +1044,19 @@ def rotary(x, freqs, positions=None, layout="half", inverse=False, scale=1.0, ou
     if layout not in _ROTARY_LAYOUTS:
         raise ValueError(f"layout: {layout!r}, expected 'half' or 'pairs'")
     dt = _act_dtype(x)
-    x_stride = _heads(x, "x", (None,) * 4, dt)
+    p_x, x_stride = _heads(x, "x", _ANY, dt)
     dev = x.device
-    batch, n, heads, hd = x.shape
+    batch, n, heads, hd = shape = tuple(x.shape)
     _need(freqs, "freqs", (None,), torch.float64, dev)
     if positions is not None:
         _need(positions, "positions", (batch, n), torch.int32, dev)
     if out is None:
-        out = torch.empty((batch, n, heads, hd), dtype=dt, device=dev)
-    y_stride = _heads(out, "out", tuple(x.shape), dt, dev)
+        out = torch.empty(shape, dtype=dt, device=dev)
+    p_y, y_stride = _heads(out, "out", shape, dt, dev)
     _gpu(dev)
     _call(dev, "hcmix_rotary", batch * n, heads, hd, 2 * freqs.numel(), _ROTARY_LAYOUTS[layout],
-          int(bool(inverse)), _dtype_code(x), _ptr(x), x_stride, _ptr(positions), n, _ptr(freqs),
-          float(scale), _ptr(out), y_stride)
+          int(bool(inverse)), HCMIX_BF16 if dt is torch.bfloat16 else HCMIX_F32, p_x, x_stride,
+          _ptr(positions), n, _ptr(freqs), float(scale), p_y, y_stride)
     return out
 
 
@@ -1057,14 +1065,14 @@ def _grouped_operands(q, k, v, lengths):
         raise ValueError("q: expected a [batch, n, heads, head_dim] tensor")
     bf = torch.bfloat16
     batch, n_q, q_heads, hd = q.shape
-    qs = _heads(q, "q", (None,) * 4, bf)
+    p_q = _heads(q, "q", _ANY, bf)
     dev = q.device
-    ks = _heads(k, "k", (batch, None, None, hd), bf, dev)
-    n_k, kv_heads = k.shape[1:3]
-    vs = _heads(v, "v", (batch, n_k, kv_heads, hd), bf, dev)
+    p_k = _heads(k, "k", (batch, None, None, hd), bf, dev)
+    _, n_k, kv_heads, _ = kv_shape = tuple(k.shape)
+    p_v = _heads(v, "v", kv_shape, bf, dev)
     if lengths is not None:
         _need(lengths, "lengths", (batch,), torch.int32, dev)
-    return dev, (batch, n_q, n_k, q_heads, kv_heads, hd), (qs, ks, vs)
+    return dev, (batch, n_q, n_k, q_heads, kv_heads, hd), (*p_q, *p_k, *p_v)
 
 
 def grouped_attention_forward(q, k, v, causal=True, lengths=None, scale=None, out=None, lse=None):
@@ -1075,7 +1083,7 @@ def grouped_attention_forward(q, k, v, causal=True, lengths=None, scale=None, ou
     sees keys up to i + n_k - n_q.  scale defaults to hd ** -0.5.  Returns (out
     bf16 like q, contiguous; lse fp32 [batch, q_heads, n_q]); a row that sees
     nothing gives 0 and -inf."""
-    dev, dims, (qs, ks, vs) = _grouped_operands(q, k, v, lengths)
+    dev, dims, operands = _grouped_operands(q, k, v, lengths)
     batch, n_q, _, q_heads, _, hd = dims
     if out is None:
         out = torch.empty((batch, n_q, q_heads, hd), dtype=q.dtype, device=dev)
@@ -1085,8 +1093,8 @@ def grouped_attention_forward(q, k, v, causal=True, lengths=None, scale=None, ou
     _need(lse, "lse", (batch, q_heads, n_q), torch.float32, dev)
     _gpu(dev)
     _call(dev, "hcmix_grouped_attention_forward", *dims, int(bool(causal)),
-          hd ** -0.5 if scale is None else float(scale), _ptr(lengths), _ptr(q), qs, _ptr(k), ks,
-          _ptr(v), vs, _ptr(out), _ptr(lse))
+          hd ** -0.5 if scale is None else float(scale), _ptr(lengths), *operands, _ptr(out),
+          _ptr(lse))
     return out, lse
 
 
@@ -1094,25 +1102,23 @@ def grouped_attention_backward(q, k, v, out, lse, dout, causal=True, lengths=Non
                                dq=None, dk=None, dv=None, workspace=None):
     """(dq, dk, dv) of ``grouped_attention_forward`` given its results and dout =
     dL/dout (contiguous).  dq, dk, dv may be slices of one packed buffer."""
-    dev, dims, (qs, ks, vs) = _grouped_operands(q, k, v, lengths)
+    dev, dims, operands = _grouped_operands(q, k, v, lengths)
     batch, n_q, n_k, q_heads, kv_heads, hd = dims
-    bf = torch.bfloat16
-    _need(out, "out", (batch, n_q, q_heads, hd), bf, dev)
+    bf, q_shape, kv_shape = torch.bfloat16, (batch, n_q, q_heads, hd), (batch, n_k, kv_heads, hd)
+    _need(out, "out", q_shape, bf, dev)
     _need(lse, "lse", (batch, q_heads, n_q), torch.float32, dev)
-    _need(dout, "dout", (batch, n_q, q_heads, hd), bf, dev)
-    dq, dk, dv = (torch.empty(t.shape, dtype=bf, device=dev) if g is None else g
-                  for g, t in ((dq, q), (dk, k), (dv, v)))
-    dqs = _heads(dq, "dq", tuple(q.shape), bf, dev)
-    dks = _heads(dk, "dk", tuple(k.shape), bf, dev)
-    dvs = _heads(dv, "dv", tuple(v.shape), bf, dev)
+    _need(dout, "dout", q_shape, bf, dev)
+    dq, dk, dv = (torch.empty(shape, dtype=bf, device=dev) if g is None else g
+                  for g, shape in ((dq, q_shape), (dk, kv_shape), (dv, kv_shape)))
+    grads = (*_heads(dq, "dq", q_shape, bf, dev), *_heads(dk, "dk", kv_shape, bf, dev),
+             *_heads(dv, "dv", kv_shape, bf, dev))
     _gpu(dev)
     if workspace is None:
         nbytes = load().hcmix_grouped_attention_backward_workspace_bytes(*dims)
         workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=dev)
     _call(dev, "hcmix_grouped_attention_backward", *dims, int(bool(causal)),
-          hd ** -0.5 if scale is None else float(scale), _ptr(lengths), _ptr(q), qs, _ptr(k), ks,
-          _ptr(v), vs, _ptr(out), _ptr(lse), _ptr(dout), _ptr(dq), dqs, _ptr(dk), dks, _ptr(dv),
-          dvs, _ptr(workspace), _workspace_bytes(workspace, dev))
+          hd ** -0.5 if scale is None else float(scale), _ptr(lengths), *operands, _ptr(out),
+          _ptr(lse), _ptr(dout), *grads, _ptr(workspace), _workspace_bytes(workspace, dev))
     return dq, dk, dv
 
 
@@ -1148,17 +1154,17 @@ def kv_cache_append(k, v, positions, cache, capacity, counts=None):
     dropped; tokens at `capacity` and behind are left out."""
     if not isinstance(k, torch.Tensor) or k.dim() != 4:
         raise ValueError("k: expected a [batch, tokens, kv_heads, head_dim] tensor")
-    ks = _heads(k, "k", (None,) * 4, torch.bfloat16)
+    p_k = _heads(k, "k", _ANY, torch.bfloat16)
     dev = k.device
-    batch, tokens, kv_heads, hd = k.shape
-    vs = _heads(v, "v", tuple(k.shape), torch.bfloat16, dev)
+    batch, tokens, kv_heads, hd = shape = tuple(k.shape)
+    p_v = _heads(v, "v", shape, torch.bfloat16, dev)
     _need(positions, "positions", (batch,), torch.int32, dev)
     if counts is not None:
         _need(counts, "counts", (batch,), torch.int32, dev)
     _cache(cache, dev)
     _gpu(dev)
-    _call(dev, "hcmix_kv_cache_append", batch, capacity, kv_heads, hd, tokens, _ptr(k), ks,
-          _ptr(v), vs, _ptr(positions), _ptr(counts), _ptr(cache), _bytes(cache))
+    _call(dev, "hcmix_kv_cache_append", batch, capacity, kv_heads, hd, tokens, *p_k, *p_v,
+          _ptr(positions), _ptr(counts), _ptr(cache), _bytes(cache))
     return cache
 
 
@@ -1190,14 +1196,14 @@ def kv_cache_attention(q, lengths, cache, capacity, kv_heads, scale=None, max_le
     max_length: how long sequences are expected to be (default: capacity)."""
     if not isinstance(q, torch.Tensor) or q.dim() != 4:
         raise ValueError("q: expected a [batch, tokens, q_heads, head_dim] tensor")
-    qs = _heads(q, "q", (None,) * 4, torch.bfloat16)
+    p_q = _heads(q, "q", _ANY, torch.bfloat16)
     dev = q.device
-    batch, tokens, q_heads, hd = q.shape
+    batch, tokens, q_heads, hd = shape = tuple(q.shape)
     _need(lengths, "lengths", (batch,), torch.int32, dev)
     _cache(cache, dev)
     if out is None:
-        out = torch.empty((batch, tokens, q_heads, hd), dtype=torch.bfloat16, device=dev)
-    _need(out, "out", (batch, tokens, q_heads, hd), torch.bfloat16, dev)
+        out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    _need(out, "out", shape, torch.bfloat16, dev)
     _gpu(dev)
     longest = capacity if max_length is None else max_length
     if workspace is None:
@@ -1206,7 +1212,7 @@ def kv_cache_attention(q, lengths, cache, capacity, kv_heads, scale=None, max_le
         if nbytes:
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     _call(dev, "hcmix_kv_cache_attention", batch, capacity, q_heads, kv_heads, hd, tokens,
-          hd ** -0.5 if scale is None else float(scale), _ptr(q), qs, _ptr(lengths), longest,
+          hd ** -0.5 if scale is None else float(scale), *p_q, _ptr(lengths), longest,
           _ptr(cache), _bytes(cache), _ptr(out), _ptr(workspace), _workspace_bytes(workspace, dev))
     return out
 
