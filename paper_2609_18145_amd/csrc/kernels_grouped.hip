@@ -272,10 +272,10 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_fwd_kernel(GroupedArgs a) {
 // but out is rounded to bf16, and dS = P (dP - D) cancels the more the fewer keys
 // share a row: a row that sees one key has dS = 0, and got 2^-9 |dout| |out|
 // instead (dq and dk of windows of 10 keys were 0.0046 off in all, 0.0024 so).
-// So tiles whose rows see at most GA_EXACT_KEYS keys take the first form; with
-// more, the rounding of out adds less than a tenth to that of dS.
+// So blocks whose rows see no more keys than the four buffers hold, 128, take the
+// first form; with more, the rounding of out adds less than a tenth to that of
+// dS.
 // ---------------------------------------------------------------------------
-constexpr int GA_EXACT_KEYS = 128;
 constexpr int GA_STEP = 32;         // rows of a streamed tile
 constexpr int GA_BUFS = 4;
 
@@ -311,6 +311,7 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) 
   load(Const<0>(), 0);
   load(Const<1>(), 1);
   load(Const<2>(), 2);
+  load(Const<3>(), 3);
   bf16x8 qf[D / 16], of[D / 16];
   ga_rows<D>(qf, a.q + (size_t)it.b * a.n_q * a.q_stride + (size_t)it.h * D, a.q_stride, q0, a.n_q, lane);
   ga_rows<D>(of, a.dout + (size_t)it.b * a.n_q * os + (size_t)it.h * D, os, q0, a.n_q, lane);
@@ -318,39 +319,37 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) 
   // keys that this lane's query sees, and its statistics
   const int seen = a.causal ? min(len, q0 + (lane & 31) + 1 + off) : len;
   float start = -INFINITY, d = 0.f;
-  if (q0 < a.n_q) {                       // wave-uniform
-    if (q0 + (lane & 31) < a.n_q) {
-      const float lse = a.lse[((size_t)it.b * a.q_heads + it.h) * a.n_q + q0 + (lane & 31)];
-      start = lse == -INFINITY ? -INFINITY : -lse / a.scale;
-    }
-    if (wave_end <= GA_EXACT_KEYS) {      // wave-uniform
-      for (int k0 = 0; k0 < wave_end; k0 += 32) {
-        bf16x8 kf[D / 16], vf[D / 16];
-        ga_rows<D>(kf, kb, a.k_stride, k0, len, lane);
-        ga_rows<D>(vf, vb, a.v_stride, k0, len, lane);
-        f32x16 s = {}, dp = {};
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ks++) {
-          s = mfma32(kf[ks], qf[ks], s);
-          dp = mfma32(vf[ks], of[ks], dp);
-        }
-#pragma unroll
-        for (int e = 0; e < 16; e++) {
-          const float p = __builtin_amdgcn_exp2f((s[e] + start) * sc);
-          d += k0 + 8 * (e >> 2) + 4 * half + (e & 3) < seen ? p * dp[e] : 0.f;
-        }
-      }
-    } else {
-      bf16x8 xf[D / 16];
-      ga_rows<D>(xf, a.out + (size_t)it.b * a.n_q * os + (size_t)it.h * D, os, q0, a.n_q, lane);
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ks++)
-#pragma unroll
-        for (int e = 0; e < 8; e++) d += (float)xf[ks][e] * (float)of[ks][e];
-    }
-    d += __shfl_xor(d, 32);
-    a.stats[ga_stats(it.b * a.q_heads + it.h, a.n_q, q0) + lane] = half ? -d : start;
+  bf16x8 xf[D / 16];
+  if (tiles > GA_BUFS) ga_rows<D>(xf, a.out + (size_t)it.b * a.n_q * os + (size_t)it.h * D, os, q0, a.n_q, lane);
+  if (q0 + (lane & 31) < a.n_q) {
+    const float lse = a.lse[((size_t)it.b * a.q_heads + it.h) * a.n_q + q0 + (lane & 31)];
+    start = lse == -INFINITY ? -INFINITY : -lse / a.scale;
   }
+  wait_vmcnt<0>();
+  __syncthreads();
+  if (tiles > GA_BUFS) {                  // block-uniform
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ks++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) d += (float)xf[ks][e] * (float)of[ks][e];
+  } else {
+    for (int t = 0; t < mine; t++) {
+      f32x16 s = {}, dp = {};
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ks++) {
+        s = mfma32(ga_frag<GA_STEP>(sK[t], 0, 16 * ks, lane), qf[ks], s);
+        dp = mfma32(ga_frag<GA_STEP>(sV[t], 0, 16 * ks, lane), of[ks], dp);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        const float p = __builtin_amdgcn_exp2f((s[e] + start) * sc);
+        d += t * GA_STEP + 8 * (e >> 2) + 4 * half + (e & 3) < seen ? p * dp[e] : 0.f;
+      }
+    }
+  }
+  d += __shfl_xor(d, 32);
+  if (q0 < a.n_q)
+    a.stats[ga_stats(it.b * a.q_heads + it.h, a.n_q, q0) + lane] = half ? -d : start;
   f32x16 start16, d16;
 #pragma unroll
   for (int e = 0; e < 16; e++) {
@@ -373,7 +372,7 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) 
     if (t + 2 < tiles) wait_vmcnt<2 * TileDma<D, GA_STEP>::PER>();
     else wait_vmcnt<0>();
     __syncthreads();
-    load(Const<(buf + 3) % GA_BUFS>(), t + 3);
+    if (t) load(Const<(buf + 3) % GA_BUFS>(), t + 3);
     if (t >= mine) return;                // wave-uniform
     if ((t + 1) * GA_STEP > full_end) {
       asm volatile("; tile with keys that some query does not see");   // no selects elsewhere
@@ -395,8 +394,6 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) 
   };
   if (tiles) {
     f32x16 s, dp, s2, dp2;
-    wait_vmcnt<0>();
-    __syncthreads();
     scores(Const<0>(), s, dp);
     for (int t = 0; t < tiles; t += 4) {
       turn(Const<0>(), t, s, dp, s2, dp2);
@@ -607,12 +604,14 @@ hipError_t ga_forward(const GroupedArgs& a, hipStream_t st) {
   return hipSuccess;
 }
 
-// Blocks that share a key tile: as many as give the chip two blocks per CU, each
-// with four query tiles at least.
+// Blocks that share a key tile where the tiles are fewer than the CUs: as many as
+// give the chip two blocks per CU, each with four query tiles at least.  (64 x
+// 256, two key/value heads, 256 blocks: 26.8 us and 7.4 for the join with two
+// parts.)
 int ga_parts(int64_t batch, int64_t n_q, int64_t n_k, int q_heads, int kv_heads) {
   const int64_t blocks = batch * kv_heads * ga_tiles((int)n_k);
   const int64_t steps = (n_q + GA_STEP - 1) / GA_STEP * (q_heads / kv_heads);
-  const int64_t want = 512 / blocks, most = steps / 4;
+  const int64_t want = blocks < 256 ? 512 / blocks : 1, most = steps / 4;
   const int64_t p = want < most ? want : most;
   return p < 1 ? 1 : p > 32 ? 32 : (int)p;
 }
