@@ -264,9 +264,8 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_fwd_kernel(GroupedArgs a) {
 // buffers in LDS, three ahead, and carry the next tile's S and dP while the
 // vector unit works on this one's.
 //
-// With lanes and registers as in the forward, S and dP start from -lse / scale
-// and -D instead of 0, so that P = exp2(S scale log2 e) and dS = P dP need no
-// subtraction.  A row that sees nothing starts from -inf: its P is 0.
+// With lanes and registers as in the forward, P = exp2((S - lse / scale) scale
+// log2 e); a row that sees nothing takes -inf for -lse: its P is 0.
 //
 // D = sum_j P_j dP_j = dout . out.  The second form is one pass over two rows,
 // but out is rounded to bf16, and dS = P (dP - D) cancels the more the fewer keys
@@ -350,17 +349,12 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) 
   d += __shfl_xor(d, 32);
   if (q0 < a.n_q)
     a.stats[ga_stats(it.b * a.q_heads + it.h, a.n_q, q0) + lane] = half ? -d : start;
-  f32x16 start16, d16;
-#pragma unroll
-  for (int e = 0; e < 16; e++) {
-    start16[e] = start;
-    d16[e] = -d;
-  }
+  start *= sc;                            // -inf stays
   f32x16 gq[D / 32] = {};
   auto scores = [&](auto buf, f32x16& s, f32x16& dp) {
     const bf16 *tk = sK[buf], *tv = sV[buf];
-    s = start16;
-    dp = d16;
+    s = f32x16{};
+    dp = f32x16{};
 #pragma unroll
     for (int ks = 0; ks < D / 16; ks++) {
       s = mfma32(ga_frag<GA_STEP>(tk, 0, 16 * ks, lane), qf[ks], s);
@@ -382,7 +376,7 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) 
     }
     scores(Const<(buf + 1) % GA_BUFS>(), s_next, dp_next);
 #pragma unroll
-    for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(s[e] * sc) * dp[e];
+    for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], sc, start)) * (dp[e] - d);
     const bf16* tk = sK[buf];
 #pragma unroll
     for (int mm = 0; mm < 2; mm++) {
@@ -413,6 +407,11 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) 
 // the query tiles that see them of the group's heads one after the other.  Where
 // the key tiles are too few for the chip, a.parts blocks share that sequence of
 // query tiles and leave fp32 sums, which ga_join_kernel adds in order.
+// A lane's 16 rows have statistics of their own, read from LDS.  For head
+// dimension 64 S and dP start from them instead of 0, which saves the vector unit
+// its subtractions (8 x 4096, 16 heads over 4: 980 us for the whole backward, 1008
+// without); for 128 the registers that hold them a turn ahead cost more (1046 us
+// with 8 heads over 2, 1022 without).
 template <int D>
 __global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(GroupedArgs a) {
   __shared__ __attribute__((aligned(1024))) bf16 sQ[GA_BUFS][GA_STEP * D], sO[GA_BUFS][GA_STEP * D];
@@ -433,6 +432,7 @@ __global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(
   ga_rows<D>(kf, a.k + (size_t)it.b * a.n_k * a.k_stride + (size_t)it.h * D, a.k_stride, j0, len, lane);
   ga_rows<D>(vf, a.v + (size_t)it.b * a.n_k * a.v_stride + (size_t)it.h * D, a.v_stride, j0, len, lane);
   f32x16 dk[D / 32] = {}, dv[D / 32] = {};
+  constexpr bool PRESET = D == 64;
   const float sc = a.scale * GA_LOG2E;
   // the query tiles that see any of the block's keys: `per` of each head from
   // `first` on; this block's are steps lo .. hi - 1 of them all
@@ -457,16 +457,20 @@ __global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(
   };
   auto scores = [&](auto buf, f32x16& s, f32x16& dp) {
     const bf16 *tq = sQ[buf], *to = sO[buf];
-    // register e: query 8 (e / 4) + 4 half + e % 4 of the tile, key j
+    if constexpr (PRESET) {
 #pragma unroll
-    for (int g = 0; g < 4; g++) {
-      const f32x4 l4 = *(const f32x4*)(sS[buf] + 8 * g + 4 * half);
-      const f32x4 d4 = *(const f32x4*)(sS[buf] + 32 + 8 * g + 4 * half);
+      for (int g = 0; g < 4; g++) {
+        const f32x4 l4 = *(const f32x4*)(sS[buf] + 8 * g + 4 * half);
+        const f32x4 d4 = *(const f32x4*)(sS[buf] + 32 + 8 * g + 4 * half);
 #pragma unroll
-      for (int r = 0; r < 4; r++) {
-        s[4 * g + r] = l4[r];
-        dp[4 * g + r] = d4[r];
+        for (int r = 0; r < 4; r++) {
+          s[4 * g + r] = l4[r];
+          dp[4 * g + r] = d4[r];
+        }
       }
+    } else {
+      s = f32x16{};
+      dp = f32x16{};
     }
 #pragma unroll
     for (int ks = 0; ks < D / 16; ks++) {
@@ -489,10 +493,24 @@ __global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(
         if (8 * (e >> 2) + 4 * half + (e & 3) < from) s[e] = -INFINITY;
     }
     scores(Const<(buf + 1) % GA_BUFS>(), s_next, dp_next);
+    if constexpr (PRESET) {
 #pragma unroll
-    for (int e = 0; e < 16; e++) {
-      s[e] = __builtin_amdgcn_exp2f(s[e] * sc);
-      dp[e] *= s[e];
+      for (int e = 0; e < 16; e++) {
+        s[e] = __builtin_amdgcn_exp2f(s[e] * sc);
+        dp[e] *= s[e];
+      }
+    } else {
+#pragma unroll
+      for (int g = 0; g < 4; g++) {
+        const f32x4 l4 = *(const f32x4*)(sS[buf] + 8 * g + 4 * half);
+        const f32x4 d4 = *(const f32x4*)(sS[buf] + 32 + 8 * g + 4 * half);
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+          const float p = __builtin_amdgcn_exp2f((s[4 * g + r] + l4[r]) * sc);
+          s[4 * g + r] = p;
+          dp[4 * g + r] = p * (dp[4 * g + r] + d4[r]);
+        }
+      }
     }
     const bf16 *tq = sQ[buf], *to = sO[buf];
 #pragma unroll
