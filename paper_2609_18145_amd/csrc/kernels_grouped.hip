@@ -139,15 +139,20 @@ __device__ __forceinline__ void ga_rows(bf16x8 (&f)[D / 16], const bf16* base, s
 // that times the number of keys, far from any limit), so that the rescaling of
 // what has been accumulated, and the exchange of the maximum between the two
 // lanes of a query, is a rare branch.
+//
+// KS = 2: where the blocks are fewer than the CUs, two sets of four waves share a
+// block's key tiles, one the even and one the odd ones, and join at the end (a
+// wave alone on its SIMD waits for itself: 3 x 1000, 8 heads of 128 over 2,
+// ragged: 23.7 us, 20.3 so).
 constexpr float GA_SLACK = 8.f;
 
-template <int D>
-__global__ __launch_bounds__(GA_THREADS, 2) void ga_fwd_kernel(GroupedArgs a) {
-  __shared__ __attribute__((aligned(1024))) bf16 sK[2][GA_TILE * D], sV[2][GA_TILE * D];
+template <int D, int KS>
+__global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
+  __shared__ __attribute__((aligned(1024))) bf16 sKV[KS][2][2][GA_TILE * D];   // keys, values
   Item it;
   if (!ga_item(a.batch, a.q_heads, (a.n_q + GA_ROWS - 1) / GA_ROWS, a.causal, &it)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = wave_index<GA_THREADS / 64>();
+  const int wave = wave_index<GA_THREADS * KS / 64>() & 3, set = wave_index<GA_THREADS * KS / 64>() >> 2;
   const int kvh = it.h / a.group, len = ga_length(a, it.b), off = a.n_k - a.n_q;
   const int blk0 = it.tile * GA_ROWS, q0 = blk0 + 32 * wave;
   const bf16* qb = a.q + (size_t)it.b * a.n_q * a.q_stride + (size_t)it.h * D;
@@ -157,14 +162,25 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_fwd_kernel(GroupedArgs a) {
   const int blk_end = a.causal ? min(len, blk0 + GA_ROWS + off) : len;
   const int wave_end = a.causal ? min(len, q0 + 32 + off) : len;
   const int full_end = a.causal ? min(len, q0 + 1 + off) : len;
-  const int tiles = blk_end > 0 ? (blk_end + GA_TILE - 1) / GA_TILE : 0;
-  const int mine = q0 < a.n_q && wave_end > 0 ? (wave_end + GA_TILE - 1) / GA_TILE : 0;
+  // tiles of the block, of this set (tile t of it is tile t KS + set), that this wave sees
+  const int all = blk_end > 0 ? (blk_end + GA_TILE - 1) / GA_TILE : 0;
+  const int turns = (all + KS - 1) / KS, tiles = (all - set + KS - 1) / KS;
+  const int seen = q0 < a.n_q && wave_end > 0 ? (wave_end + GA_TILE - 1) / GA_TILE : 0;
+  const int mine = (seen - set + KS - 1) / KS;
+  bf16(*sK)[GA_TILE * D] = sKV[set][0];
+  bf16(*sV)[GA_TILE * D] = sKV[set][1];
   bf16x8 qf[D / 16];
   ga_rows<D>(qf, qb, a.q_stride, q0, a.n_q, lane);
   f32x16 o[D / 32] = {};
   const float sc = a.scale * GA_LOG2E;
   float m = -3e38f, l = 0.f, limit = -INFINITY;      // limit: the score from which m grows
   const TileDma<D, GA_TILE> dk(wave, lane, a.k_stride), dv(wave, lane, a.v_stride);
+  auto load_k = [&](int t, bf16* to) {
+    if (t < tiles) dk.load(kb, a.k_stride, (t * KS + set) * GA_TILE, len, to);
+  };
+  auto load_v = [&](int t, bf16* to) {
+    if (t < tiles) dv.load(vb, a.v_stride, (t * KS + set) * GA_TILE, len, to);
+  };
   auto scores = [&](const bf16* tk, f32x16 (&r)[2]) {
 #pragma unroll
     for (int kt = 0; kt < 2; kt++) {
@@ -177,10 +193,10 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_fwd_kernel(GroupedArgs a) {
   auto turn = [&](auto buf, int t, f32x16 (&s)[2], f32x16 (&next)[2]) {   // buf: t % 2
     wait_dma();
     __syncthreads();
-    if (t + 2 < tiles) dk.load(kb, a.k_stride, (t + 2) * GA_TILE, len, sK[buf]);
-    if (t + 1 < tiles) dv.load(vb, a.v_stride, (t + 1) * GA_TILE, len, sV[buf ^ 1]);
+    load_k(t + 2, sK[buf]);
+    load_v(t + 1, sV[buf ^ 1]);
     if (t >= mine) return;               // wave-uniform
-    const int k0 = t * GA_TILE;
+    const int k0 = (t * KS + set) * GA_TILE;
     if (k0 + GA_TILE > full_end) {
       asm volatile("; tile with keys that some query does not see");   // no selects elsewhere
       // register e of a lane: key k0 + 32 kt + 8 (e / 4) + 4 half + e % 4
@@ -232,18 +248,46 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_fwd_kernel(GroupedArgs a) {
       }
     }
   };
-  if (tiles) {
+  if (turns) {
     f32x16 s[2], next[2];
-    dk.load(kb, a.k_stride, 0, len, sK[0]);
-    dv.load(vb, a.v_stride, 0, len, sV[0]);
-    if (tiles > 1) dk.load(kb, a.k_stride, GA_TILE, len, sK[1]);
+    load_k(0, sK[0]);
+    load_v(0, sV[0]);
+    load_k(1, sK[1]);
     wait_dma();
     __syncthreads();
     scores(sK[0], s);
-    for (int t = 0; t < tiles; t += 2) {
+    for (int t = 0; t < turns; t += 2) {
       turn(Const<0>(), t, s, next);
-      if (t + 1 < tiles) turn(Const<1>(), t + 1, next, s);
+      if (t + 1 < turns) turn(Const<1>(), t + 1, next, s);
     }
+  }
+  if constexpr (KS == 2) {
+    // the second set's sums to the first, through the tiles' place: [wave][register quad][lane]
+    static_assert(sizeof(sKV) >= 4 * (D / 8 + 1) * 64 * sizeof(f32x4), "");
+    f32x4* to = (f32x4*)sKV + wave * (D / 8 + 1) * 64 + lane;
+    __syncthreads();
+    if (set) {
+#pragma unroll
+      for (int d = 0; d < D / 32; d++)
+#pragma unroll
+        for (int g = 0; g < 4; g++)
+          to[(4 * d + g) * 64] = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+      to[D / 8 * 64] = f32x4{m, l, 0.f, 0.f};
+    }
+    __syncthreads();
+    if (set) return;
+    const f32x4 ml = to[D / 8 * 64];
+    const float mn = fmaxf(m, ml[0]), x = __builtin_amdgcn_exp2f(m - mn), y = __builtin_amdgcn_exp2f(ml[0] - mn);
+    m = mn;
+    l = l * x + ml[1] * y;
+#pragma unroll
+    for (int d = 0; d < D / 32; d++)
+#pragma unroll
+      for (int g = 0; g < 4; g++) {
+        const f32x4 v = to[(4 * d + g) * 64];
+#pragma unroll
+        for (int r = 0; r < 4; r++) o[d][4 * g + r] = o[d][4 * g + r] * x + v[r] * y;
+      }
   }
   if (q0 >= a.n_q) return;
   l += __shfl_xor(l, 32);
@@ -284,13 +328,13 @@ __device__ __forceinline__ size_t ga_stats(int bh, int n_q, int row0) {
   return ((size_t)bh * ((n_q + 31) / 32) + row0 / 32) * 64;
 }
 
-template <int D>
-__global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) {
-  __shared__ __attribute__((aligned(1024))) bf16 sK[GA_BUFS][GA_STEP * D], sV[GA_BUFS][GA_STEP * D];
+template <int D, int KS>
+__global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_q_kernel(GroupedArgs a) {
+  __shared__ __attribute__((aligned(1024))) bf16 sKV[KS][2][GA_BUFS][GA_STEP * D];   // keys, values
   Item it;
   if (!ga_item(a.batch, a.q_heads, (a.n_q + GA_ROWS - 1) / GA_ROWS, a.causal, &it)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = wave_index<GA_THREADS / 64>();
+  const int wave = wave_index<GA_THREADS * KS / 64>() & 3, set = wave_index<GA_THREADS * KS / 64>() >> 2;
   const int kvh = it.h / a.group, len = ga_length(a, it.b), off = a.n_k - a.n_q;
   const int blk0 = it.tile * GA_ROWS, q0 = blk0 + 32 * wave;
   const size_t os = (size_t)a.q_heads * D;
@@ -299,13 +343,18 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) 
   const int blk_end = a.causal ? min(len, blk0 + GA_ROWS + off) : len;
   const int wave_end = a.causal ? min(len, q0 + 32 + off) : len;
   const int full_end = a.causal ? min(len, q0 + 1 + off) : len;
-  const int tiles = blk_end > 0 ? (blk_end + GA_STEP - 1) / GA_STEP : 0;
-  const int mine = q0 < a.n_q && wave_end > 0 ? (wave_end + GA_STEP - 1) / GA_STEP : 0;
+  // tiles as in the forward
+  const int all = blk_end > 0 ? (blk_end + GA_STEP - 1) / GA_STEP : 0;
+  const int turns = (all + KS - 1) / KS, tiles = (all - set + KS - 1) / KS;
+  const int wave_tiles = q0 < a.n_q && wave_end > 0 ? (wave_end + GA_STEP - 1) / GA_STEP : 0;
+  const int mine = (wave_tiles - set + KS - 1) / KS;
+  bf16(*sK)[GA_STEP * D] = sKV[set][0];
+  bf16(*sV)[GA_STEP * D] = sKV[set][1];
   const TileDma<D, GA_STEP> dk(wave, lane, a.k_stride), dv(wave, lane, a.v_stride);
   auto load = [&](auto buf, int t) {      // buf: t % GA_BUFS
     if (t >= tiles) return;
-    dk.load(kb, a.k_stride, t * GA_STEP, len, sK[buf]);
-    dv.load(vb, a.v_stride, t * GA_STEP, len, sV[buf]);
+    dk.load(kb, a.k_stride, (t * KS + set) * GA_STEP, len, sK[buf]);
+    dv.load(vb, a.v_stride, (t * KS + set) * GA_STEP, len, sV[buf]);
   };
   load(Const<0>(), 0);
   load(Const<1>(), 1);
@@ -319,14 +368,14 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) 
   const int seen = a.causal ? min(len, q0 + (lane & 31) + 1 + off) : len;
   float start = -INFINITY, d = 0.f;
   bf16x8 xf[D / 16];
-  if (tiles > GA_BUFS) ga_rows<D>(xf, a.out + (size_t)it.b * a.n_q * os + (size_t)it.h * D, os, q0, a.n_q, lane);
+  if (all > GA_BUFS) ga_rows<D>(xf, a.out + (size_t)it.b * a.n_q * os + (size_t)it.h * D, os, q0, a.n_q, lane);
   if (q0 + (lane & 31) < a.n_q) {
     const float lse = a.lse[((size_t)it.b * a.q_heads + it.h) * a.n_q + q0 + (lane & 31)];
     start = lse == -INFINITY ? -INFINITY : -lse / a.scale;
   }
   wait_vmcnt<0>();
   __syncthreads();
-  if (tiles > GA_BUFS) {                  // block-uniform
+  if (all > GA_BUFS) {                    // block-uniform
 #pragma unroll
     for (int ks = 0; ks < D / 16; ks++)
 #pragma unroll
@@ -342,12 +391,18 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) 
 #pragma unroll
       for (int e = 0; e < 16; e++) {
         const float p = __builtin_amdgcn_exp2f((s[e] + start) * sc);
-        d += t * GA_STEP + 8 * (e >> 2) + 4 * half + (e & 3) < seen ? p * dp[e] : 0.f;
+        d += (t * KS + set) * GA_STEP + 8 * (e >> 2) + 4 * half + (e & 3) < seen ? p * dp[e] : 0.f;
       }
+    }
+    if constexpr (KS == 2) {              // the other set's share
+      __shared__ float sD[2][4][64];
+      sD[set][wave][lane] = d;
+      __syncthreads();
+      d += sD[set ^ 1][wave][lane];
     }
   }
   d += __shfl_xor(d, 32);
-  if (q0 < a.n_q)
+  if (q0 < a.n_q && !set)
     a.stats[ga_stats(it.b * a.q_heads + it.h, a.n_q, q0) + lane] = half ? -d : start;
   start *= sc;                            // -inf stays
   f32x16 gq[D / 32] = {};
@@ -368,11 +423,11 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) 
     __syncthreads();
     if (t) load(Const<(buf + 3) % GA_BUFS>(), t + 3);
     if (t >= mine) return;                // wave-uniform
-    if ((t + 1) * GA_STEP > full_end) {
+    if ((t * KS + set + 1) * GA_STEP > full_end) {
       asm volatile("; tile with keys that some query does not see");   // no selects elsewhere
 #pragma unroll
       for (int e = 0; e < 16; e++)
-        if (t * GA_STEP + 8 * (e >> 2) + 4 * half + (e & 3) >= seen) s[e] = -INFINITY;
+        if ((t * KS + set) * GA_STEP + 8 * (e >> 2) + 4 * half + (e & 3) >= seen) s[e] = -INFINITY;
     }
     scores(Const<(buf + 1) % GA_BUFS>(), s_next, dp_next);
 #pragma unroll
@@ -386,15 +441,36 @@ __global__ __launch_bounds__(GA_THREADS, 2) void ga_bwd_q_kernel(GroupedArgs a) 
         gq[dt] = mfma32(ga_trfrag<GA_STEP>(tk, 16 * mm, 32 * dt, lane), sf, gq[dt]);
     }
   };
-  if (tiles) {
+  if (turns) {
     f32x16 s, dp, s2, dp2;
     scores(Const<0>(), s, dp);
-    for (int t = 0; t < tiles; t += 4) {
+    for (int t = 0; t < turns; t += 4) {
       turn(Const<0>(), t, s, dp, s2, dp2);
-      if (t + 1 < tiles) turn(Const<1>(), t + 1, s2, dp2, s, dp);
-      if (t + 2 < tiles) turn(Const<2>(), t + 2, s, dp, s2, dp2);
-      if (t + 3 < tiles) turn(Const<3>(), t + 3, s2, dp2, s, dp);
+      if (t + 1 < turns) turn(Const<1>(), t + 1, s2, dp2, s, dp);
+      if (t + 2 < turns) turn(Const<2>(), t + 2, s, dp, s2, dp2);
+      if (t + 3 < turns) turn(Const<3>(), t + 3, s2, dp2, s, dp);
     }
+  }
+  if constexpr (KS == 2) {                // as in the forward
+    static_assert(sizeof(sKV) >= 4 * D / 8 * 64 * sizeof(f32x4), "");
+    f32x4* to = (f32x4*)sKV + wave * (D / 8) * 64 + lane;
+    __syncthreads();
+    if (set)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+        for (int g = 0; g < 4; g++)
+          to[(4 * dt + g) * 64] = f32x4{gq[dt][4 * g], gq[dt][4 * g + 1], gq[dt][4 * g + 2], gq[dt][4 * g + 3]};
+    __syncthreads();
+    if (set) return;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+      for (int g = 0; g < 4; g++) {
+        const f32x4 v = to[(4 * dt + g) * 64];
+#pragma unroll
+        for (int r = 0; r < 4; r++) gq[dt][4 * g + r] += v[r];
+      }
   }
   if (q0 >= a.n_q) return;
   bf16* dqb = a.dq + ((size_t)it.b * a.n_q + q0) * a.dq_stride + (size_t)it.h * D;
@@ -607,6 +683,9 @@ GroupedArgs ga_slice(const GroupedArgs& a, int64_t b0, int64_t nb) {
 }
 
 constexpr int64_t GA_MAX_BLOCKS = 1 << 23;     // of a launch: below 2^32 threads
+// Sets of four waves that share a block's tiles of keys: two where a CU has one
+// block at most.
+int ga_sets(int64_t blocks) { return blocks <= 256 ? 2 : 1; }
 int64_t ga_tiles(int n) { return (n + GA_ROWS - 1) / GA_ROWS; }
 
 template <int D>
@@ -615,7 +694,10 @@ hipError_t ga_forward(const GroupedArgs& a, hipStream_t st) {
   const int64_t most = GA_MAX_BLOCKS / per > 0 ? GA_MAX_BLOCKS / per : 1;
   for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
     const int64_t nb = a.batch - b0 < most ? a.batch - b0 : most;
-    ga_fwd_kernel<D><<<(int)(nb * per), GA_THREADS, 0, st>>>(ga_slice(a, b0, nb));
+    if (ga_sets(nb * per) == 2)
+      ga_fwd_kernel<D, 2><<<(int)(nb * per), 2 * GA_THREADS, 0, st>>>(ga_slice(a, b0, nb));
+    else
+      ga_fwd_kernel<D, 1><<<(int)(nb * per), GA_THREADS, 0, st>>>(ga_slice(a, b0, nb));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -647,7 +729,10 @@ hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
   for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
     const int64_t nb = a.batch - b0 < most ? a.batch - b0 : most;
     const GroupedArgs s = ga_slice(a, b0, nb);
-    ga_bwd_q_kernel<D><<<(int)(nb * q), GA_THREADS, 0, st>>>(s);
+    if (ga_sets(nb * q) == 2)
+      ga_bwd_q_kernel<D, 2><<<(int)(nb * q), 2 * GA_THREADS, 0, st>>>(s);
+    else
+      ga_bwd_q_kernel<D, 1><<<(int)(nb * q), GA_THREADS, 0, st>>>(s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     ga_bwd_kv_kernel<D><<<(int)(nb * kv), GA_THREADS, 0, st>>>(s);

@@ -95,6 +95,33 @@ def test_long_window_sampled():
         within(name, g[i][:, :, 2 if i == 0 else 1:], ref[i], bounds[i])
 
 
+@pytest.mark.parametrize("batch,n_q,n_k,heads,kv,hd,causal", [
+    (40, 100, 100, 8, 4, 64, True), (40, 70, 200, 8, 8, 128, False), (3, 1500, 1500, 16, 2, 64, True),
+    (44, 129, 257, 6, 3, 128, True)])
+def test_more_blocks_than_compute_units_sampled(batch, n_q, n_k, heads, kv, hd, causal):
+    """Ragged batches that fill the chip several times; three (sequence, group) pairs."""
+    print(f"case: {batch} {n_q} {n_k} {heads} {kv} {hd} {causal}", flush=True)
+    q, k, v, do = draw(batch, n_q, n_k, heads, kv, hd, seed=batch)
+    lengths = [(7 * b + 1) % (n_k + 1) for b in range(batch)]
+    lengths[-1] = n_k
+    ln = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    out, lse = hcmix.grouped_attention_forward(q, k, v, causal, ln)
+    g = hcmix.grouped_attention_backward(q, k, v, out, lse, do, causal, ln)
+    per = heads // kv
+    for b, c in ((0, 0), (batch // 2, kv - 1), (batch - 1, kv // 2)):
+        hq, ck = slice(c * per, c * per + per), slice(c, c + 1)
+        s = [host(t[b:b + 1, :, h]) for t, h in ((q, hq), (k, ck), (v, ck), (do, hq))]
+        r_out, r_lse, bound = grouped.forward(*s[:3], causal, lengths[b:b + 1])
+        within("out", out[b:b + 1, :, hq], r_out, bound)
+        seen = ~np.isneginf(r_lse)
+        got = host(lse[b:b + 1, hq])
+        assert np.array_equal(~np.isneginf(got), seen)
+        assert np.abs(got[seen] - r_lse[seen]).max(initial=0.0) <= 2.0 ** -14 * 10
+        ref, bounds = grouped.backward(*s, causal, lengths[b:b + 1])
+        for i, (name, h) in enumerate((("dq", hq), ("dk", ck), ("dv", ck))):
+            within(name, g[i][b:b + 1, :, h], ref[i], bounds[i])
+
+
 @pytest.mark.parametrize("heads,kv,hd", [(4, 2, 64), (2, 2, 128)])
 def test_packed_projection_in_and_out(heads, kv, hd):
     """Slices of one packed buffer in and one packed gradient out: as apart."""
