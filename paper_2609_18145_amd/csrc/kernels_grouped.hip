@@ -316,8 +316,8 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_fwd_kernel(GroupedArgs 
 // share a row: a row that sees one key has dS = 0, and got 2^-9 |dout| |out|
 // instead (dq and dk of windows of 10 keys were 0.0046 off in all, 0.0024 so).
 // So blocks whose rows see no more keys than the four buffers hold, 128, take the
-// first form; with more, the rounding of out adds less than a tenth to that of
-// dS.
+// first form, over sum_j P_j, which lse's own rounding keeps from being 1; with
+// more, the rounding of out adds less than a tenth to that of dS.
 // ---------------------------------------------------------------------------
 constexpr int GA_STEP = 32;         // rows of a streamed tile
 constexpr int GA_BUFS = 4;
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_q_kernel(GroupedArg
   const float sc = a.scale * GA_LOG2E;
   // keys that this lane's query sees, and its statistics
   const int seen = a.causal ? min(len, q0 + (lane & 31) + 1 + off) : len;
-  float start = -INFINITY, d = 0.f;
+  float start = -INFINITY, d = 0.f, z = 0.f;
   bf16x8 xf[D / 16];
   if (all > GA_BUFS) ga_rows<D>(xf, a.out + (size_t)it.b * a.n_q * os + (size_t)it.h * D, os, q0, a.n_q, lane);
   if (q0 + (lane & 31) < a.n_q) {
@@ -390,18 +390,24 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_q_kernel(GroupedArg
       }
 #pragma unroll
       for (int e = 0; e < 16; e++) {
-        const float p = __builtin_amdgcn_exp2f((s[e] + start) * sc);
-        d += (t * KS + set) * GA_STEP + 8 * (e >> 2) + 4 * half + (e & 3) < seen ? p * dp[e] : 0.f;
+        float p = __builtin_amdgcn_exp2f((s[e] + start) * sc);
+        if ((t * KS + set) * GA_STEP + 8 * (e >> 2) + 4 * half + (e & 3) >= seen) p = 0.f;
+        d += p * dp[e];
+        z += p;
       }
     }
     if constexpr (KS == 2) {              // the other set's share
-      __shared__ float sD[2][4][64];
-      sD[set][wave][lane] = d;
+      __shared__ float2 sD[2][4][64];
+      sD[set][wave][lane] = float2{d, z};
       __syncthreads();
-      d += sD[set ^ 1][wave][lane];
+      const float2 other = sD[set ^ 1][wave][lane];
+      d += other.x;
+      z += other.y;
     }
+    z += __shfl_xor(z, 32);
   }
   d += __shfl_xor(d, 32);
+  if (z > 0.f) d /= z;
   if (q0 < a.n_q && !set)
     a.stats[ga_stats(it.b * a.q_heads + it.h, a.n_q, q0) + lane] = half ? -d : start;
   start *= sc;                            // -inf stays
