@@ -489,24 +489,26 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_q_kernel(GroupedArg
 // the query tiles that see them of the group's heads one after the other.  Where
 // the key tiles are too few for the chip, a.parts blocks share that sequence of
 // query tiles and leave fp32 sums, which ga_join_kernel adds in order.
-// A lane's 16 rows have statistics of their own, read from LDS.  For head
-// dimension 64 S and dP start from them instead of 0, which saves the vector unit
-// its subtractions (8 x 4096, 16 heads over 4: 980 us for the whole backward, 1008
-// without); for 128 the registers that hold them a turn ahead cost more (1046 us
-// with 8 heads over 2, 1022 without).
-template <int D>
-__global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(GroupedArgs a) {
-  __shared__ __attribute__((aligned(1024))) bf16 sQ[GA_BUFS][GA_STEP * D], sO[GA_BUFS][GA_STEP * D];
+// A lane's 16 rows have statistics of their own, read from LDS: S and dP start from
+// them instead of 0, which saves the vector unit its subtractions (8 x 4096, 16
+// heads of 64 over 4: 980 us for the whole backward, 1008 without).  KS as in the
+// forward, for head dimension 64 alone: with 128 a SIMD's registers hold one wave.
+template <int D, int KS>
+__global__ __launch_bounds__(GA_THREADS * KS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(GroupedArgs a) {
+  __shared__ __attribute__((aligned(1024))) bf16 sQO[KS][2][GA_BUFS][GA_STEP * D];   // queries, dout
   // a tile's statistics, four times over: every wave copies them, to keep one
   // count of loads on their way, and 64 lanes copy 1 KB
-  __shared__ __attribute__((aligned(1024))) float sS[GA_BUFS][256];
+  __shared__ __attribute__((aligned(1024))) float sST[KS][GA_BUFS][256];
   Item it;
   const int key_tiles = (a.n_k + GA_ROWS - 1) / GA_ROWS;
   if (!ga_item(a.batch, a.kv_heads, key_tiles * a.parts, false, &it)) return;
   const int part = it.tile % a.parts;
   it.tile /= a.parts;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = wave_index<GA_THREADS / 64>();
+  const int wave = wave_index<GA_THREADS * KS / 64>() & 3, set = wave_index<GA_THREADS * KS / 64>() >> 2;
+  bf16(*sQ)[GA_STEP * D] = sQO[set][0];
+  bf16(*sO)[GA_STEP * D] = sQO[set][1];
+  float(*sS)[256] = sST[set];
   const int len = ga_length(a, it.b), off = a.n_k - a.n_q;
   const int blk0 = it.tile * GA_ROWS, j0 = blk0 + 32 * wave, j = j0 + (lane & 31);
   const size_t os = (size_t)a.q_heads * D;
@@ -514,17 +516,18 @@ __global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(
   ga_rows<D>(kf, a.k + (size_t)it.b * a.n_k * a.k_stride + (size_t)it.h * D, a.k_stride, j0, len, lane);
   ga_rows<D>(vf, a.v + (size_t)it.b * a.n_k * a.v_stride + (size_t)it.h * D, a.v_stride, j0, len, lane);
   f32x16 dk[D / 32] = {}, dv[D / 32] = {};
-  constexpr bool PRESET = D == 64;
   const float sc = a.scale * GA_LOG2E;
   // the query tiles that see any of the block's keys: `per` of each head from
-  // `first` on; this block's are steps lo .. hi - 1 of them all
+  // `first` on; this block's are steps lo .. hi - 1 of them all, this set's every
+  // KS-th of those
   const int first = a.causal && blk0 - off > 0 ? (blk0 - off) / GA_STEP : 0;
   const int per = blk0 < len ? max(0, (a.n_q + GA_STEP - 1) / GA_STEP - first) : 0;
   const int lo = (int)((int64_t)per * a.group * part / a.parts);
-  const int steps = (int)((int64_t)per * a.group * (part + 1) / a.parts) - lo;
+  const int hi = (int)((int64_t)per * a.group * (part + 1) / a.parts);
+  const int turns = (hi - lo + KS - 1) / KS, steps = (hi - lo - set + KS - 1) / KS;
   const TileDma<D, GA_STEP> dq(wave, lane, a.q_stride), dout(wave, lane, os);
-  int lg = steps ? lo / per : 0, lt = lo - lg * per;      // head and tile to be loaded next
-  int ct = lt;                                            // tile to be computed next
+  int lg = per ? (lo + set) / per : 0, lt = lo + set - lg * per;   // head and tile to be loaded next
+  int ct = lt;                                                     // tile to be computed next
   auto load = [&](auto buf, int step) {                   // buf: step % GA_BUFS
     if (step >= steps) return;
     const int h = it.h * a.group + lg, i0 = (first + lt) * GA_STEP;
@@ -532,27 +535,25 @@ __global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(
     dout.load(a.dout + (size_t)it.b * a.n_q * os + (size_t)h * D, os, i0, a.n_q, sO[buf]);
     dma16_at((const bf16*)(a.stats + ga_stats(it.b * a.q_heads + h, a.n_q, i0)), 16 * (lane & 15),
              (bf16*)sS[buf]);
-    if (++lt == per) {
-      lt = 0;
-      lg++;
-    }
+#pragma unroll
+    for (int i = 0; i < KS; i++)
+      if (++lt == per) {
+        lt = 0;
+        lg++;
+      }
   };
   auto scores = [&](auto buf, f32x16& s, f32x16& dp) {
     const bf16 *tq = sQ[buf], *to = sO[buf];
-    if constexpr (PRESET) {
+    // register e: query 8 (e / 4) + 4 half + e % 4 of the tile, key j
 #pragma unroll
-      for (int g = 0; g < 4; g++) {
-        const f32x4 l4 = *(const f32x4*)(sS[buf] + 8 * g + 4 * half);
-        const f32x4 d4 = *(const f32x4*)(sS[buf] + 32 + 8 * g + 4 * half);
+    for (int g = 0; g < 4; g++) {
+      const f32x4 l4 = *(const f32x4*)(sS[buf] + 8 * g + 4 * half);
+      const f32x4 d4 = *(const f32x4*)(sS[buf] + 32 + 8 * g + 4 * half);
 #pragma unroll
-        for (int r = 0; r < 4; r++) {
-          s[4 * g + r] = l4[r];
-          dp[4 * g + r] = d4[r];
-        }
+      for (int r = 0; r < 4; r++) {
+        s[4 * g + r] = l4[r];
+        dp[4 * g + r] = d4[r];
       }
-    } else {
-      s = f32x16{};
-      dp = f32x16{};
     }
 #pragma unroll
     for (int ks = 0; ks < D / 16; ks++) {
@@ -566,7 +567,10 @@ __global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(
     __syncthreads();
     load(Const<(buf + 3) % GA_BUFS>(), step + 3);
     const int r0 = (first + ct) * GA_STEP;
-    if (++ct == per) ct = 0;
+#pragma unroll
+    for (int i = 0; i < KS; i++)
+      if (++ct == per) ct = 0;
+    if (KS > 1 && step >= steps) return;           // wave-uniform
     if (j0 + 32 > len || (a.causal && r0 + off < j0 + 31)) {
       asm volatile("; tile with keys that some query does not see");
       const int from = j >= len ? 1 << 30 : a.causal ? j - off - r0 : -1;   // first row that sees j
@@ -575,24 +579,10 @@ __global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(
         if (8 * (e >> 2) + 4 * half + (e & 3) < from) s[e] = -INFINITY;
     }
     scores(Const<(buf + 1) % GA_BUFS>(), s_next, dp_next);
-    if constexpr (PRESET) {
 #pragma unroll
-      for (int e = 0; e < 16; e++) {
-        s[e] = __builtin_amdgcn_exp2f(s[e] * sc);
-        dp[e] *= s[e];
-      }
-    } else {
-#pragma unroll
-      for (int g = 0; g < 4; g++) {
-        const f32x4 l4 = *(const f32x4*)(sS[buf] + 8 * g + 4 * half);
-        const f32x4 d4 = *(const f32x4*)(sS[buf] + 32 + 8 * g + 4 * half);
-#pragma unroll
-        for (int r = 0; r < 4; r++) {
-          const float p = __builtin_amdgcn_exp2f((s[4 * g + r] + l4[r]) * sc);
-          s[4 * g + r] = p;
-          dp[4 * g + r] = p * (dp[4 * g + r] + d4[r]);
-        }
-      }
+    for (int e = 0; e < 16; e++) {
+      s[e] = __builtin_amdgcn_exp2f(s[e] * sc);
+      dp[e] *= s[e];
     }
     const bf16 *tq = sQ[buf], *to = sO[buf];
 #pragma unroll
@@ -604,8 +594,12 @@ __global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(
         dk[d] = mfma32(ga_trfrag<GA_STEP>(tq, 16 * mm, 32 * d, lane), sf, dk[d]);
       }
     }
+    // the compiler's order for matrix products fed from LDS: with head dimension
+    // 128 a wave is alone on its SIMD (8 x 4096, 8 heads over 2: 1030 us for the
+    // backward, 977 so; 64: the same either way)
+    __builtin_amdgcn_iglp_opt(0);
   };
-  if (steps) {
+  if (turns > 0) {
     f32x16 s, dp, s2, dp2;
     load(Const<0>(), 0);
     load(Const<1>(), 1);
@@ -613,12 +607,38 @@ __global__ __launch_bounds__(GA_THREADS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(
     wait_vmcnt<0>();
     __syncthreads();
     scores(Const<0>(), s, dp);
-    for (int t = 0; t < steps; t += 4) {
+    for (int t = 0; t < turns; t += 4) {
       turn(Const<0>(), t, s, dp, s2, dp2);
-      if (t + 1 < steps) turn(Const<1>(), t + 1, s2, dp2, s, dp);
-      if (t + 2 < steps) turn(Const<2>(), t + 2, s, dp, s2, dp2);
-      if (t + 3 < steps) turn(Const<3>(), t + 3, s2, dp2, s, dp);
+      if (t + 1 < turns) turn(Const<1>(), t + 1, s2, dp2, s, dp);
+      if (t + 2 < turns) turn(Const<2>(), t + 2, s, dp, s2, dp2);
+      if (t + 3 < turns) turn(Const<3>(), t + 3, s2, dp2, s, dp);
     }
+  }
+  if constexpr (KS == 2) {               // as in the forward
+    static_assert(sizeof(sQO) >= 4 * 2 * D / 8 * 64 * sizeof(f32x4), "");
+    f32x4* to = (f32x4*)sQO + wave * (D / 4) * 64 + lane;
+    __syncthreads();
+    if (set)
+#pragma unroll
+      for (int d = 0; d < D / 32; d++)
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+          to[(8 * d + g) * 64] = f32x4{dk[d][4 * g], dk[d][4 * g + 1], dk[d][4 * g + 2], dk[d][4 * g + 3]};
+          to[(8 * d + 4 + g) * 64] = f32x4{dv[d][4 * g], dv[d][4 * g + 1], dv[d][4 * g + 2], dv[d][4 * g + 3]};
+        }
+    __syncthreads();
+    if (set) return;
+#pragma unroll
+    for (int d = 0; d < D / 32; d++)
+#pragma unroll
+      for (int g = 0; g < 4; g++) {
+        const f32x4 x = to[(8 * d + g) * 64], y = to[(8 * d + 4 + g) * 64];
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+          dk[d][4 * g + r] += x[r];
+          dv[d][4 * g + r] += y[r];
+        }
+      }
   }
   if (j0 >= a.n_k) return;
   if (a.parts > 1) {
@@ -711,13 +731,13 @@ hipError_t ga_forward(const GroupedArgs& a, hipStream_t st) {
 }
 
 // Blocks that share a key tile where the tiles are fewer than the CUs: as many as
-// give the chip two blocks per CU, each with four query tiles at least.  (64 x
-// 256, two key/value heads, 256 blocks: 26.8 us and 7.4 for the join with two
-// parts.)
-int ga_parts(int64_t batch, int64_t n_q, int64_t n_k, int q_heads, int kv_heads) {
+// the chip holds at once (two to a CU, one for head dimension 128), each with four
+// query tiles at least.  (5 x 333 x 777, 8 heads of 128 over 2: the backward took
+// 60 us with 256 blocks, 72 with 512; 4 x 1024, 16 heads of 64 over 4: 70 and 66.)
+int ga_parts(int64_t batch, int64_t n_q, int64_t n_k, int q_heads, int kv_heads, int head_dim) {
   const int64_t blocks = batch * kv_heads * ga_tiles((int)n_k);
   const int64_t steps = (n_q + GA_STEP - 1) / GA_STEP * (q_heads / kv_heads);
-  const int64_t want = blocks < 256 ? 512 / blocks : 1, most = steps / 4;
+  const int64_t want = blocks < 256 ? (head_dim == 64 ? 512 : 256) / blocks : 1, most = steps / 4;
   const int64_t p = want < most ? want : most;
   return p < 1 ? 1 : p > 32 ? 32 : (int)p;
 }
@@ -741,7 +761,14 @@ hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
       ga_bwd_q_kernel<D, 1><<<(int)(nb * q), GA_THREADS, 0, st>>>(s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    ga_bwd_kv_kernel<D><<<(int)(nb * kv), GA_THREADS, 0, st>>>(s);
+    if constexpr (D == 64) {
+      if (ga_sets(nb * kv) == 2)
+        ga_bwd_kv_kernel<D, 2><<<(int)(nb * kv), 2 * GA_THREADS, 0, st>>>(s);
+      else
+        ga_bwd_kv_kernel<D, 1><<<(int)(nb * kv), GA_THREADS, 0, st>>>(s);
+    } else {
+      ga_bwd_kv_kernel<D, 1><<<(int)(nb * kv), GA_THREADS, 0, st>>>(s);
+    }
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (a.parts > 1) {
@@ -758,7 +785,7 @@ hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
 
 size_t grouped_workspace_bytes(int64_t batch, int64_t n_q, int64_t n_k, int32_t q_heads,
                                int32_t kv_heads, int32_t head_dim) {
-  const int parts = ga_parts(batch, n_q, n_k, q_heads, kv_heads);
+  const int parts = ga_parts(batch, n_q, n_k, q_heads, kv_heads, head_dim);
   const size_t sums = parts > 1 ? (size_t)parts * 2 * batch * n_k * kv_heads * head_dim * sizeof(float) : 0;
   return (ga_stats_bytes(batch, n_q, q_heads) + sums + 255) / 256 * 256;
 }
@@ -768,7 +795,7 @@ hipError_t launch_grouped_forward(const GroupedArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_grouped_backward(GroupedArgs a, void* workspace, hipStream_t st) {
-  a.parts = ga_parts(a.batch, a.n_q, a.n_k, a.q_heads, a.kv_heads);
+  a.parts = ga_parts(a.batch, a.n_q, a.n_k, a.q_heads, a.kv_heads, a.head_dim);
   a.stats = (float*)workspace;
   a.partial = a.stats + ga_stats_bytes(a.batch, a.n_q, a.q_heads) / sizeof(float);
   return a.head_dim == 64 ? ga_backward<64>(a, st) : ga_backward<128>(a, st);
