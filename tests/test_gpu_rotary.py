@@ -77,6 +77,16 @@ def test_scaled_contexts(scaling):
     check(y, x, pos.numpy(), freqs, True, scale, False)
 
 
+def test_more_rows_than_a_grid_has_blocks():
+    """4.2 million positions: blocks that take rows more than once; the last ones."""
+    n = (1 << 22) + 7
+    x = torch.randn((1, n, 1, 2), generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    freqs, _ = hcmix.rotary_frequencies(2)
+    y = hcmix.rotary(x, freqs)
+    at = torch.tensor([0, 3, 4, 12345, (1 << 22) - 1, 1 << 22, n - 1], device="cuda")
+    check(y[:, at], x[:, at], at.cpu().numpy()[None], freqs, True, 1.0, False)
+
+
 def test_gradient_is_the_inverse_turn():
     x = torch.randn(2, 5, 3, 64, device="cuda", requires_grad=True)
     freqs, _ = hcmix.rotary_frequencies(64)
