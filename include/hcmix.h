@@ -602,7 +602,8 @@ hcmix_status hcmix_grouped_attention_forward(
  *   dq = dS k, dk = dS^T q, summed over the query heads of a group.
  * P is made again from lse.  Sums run in a fixed order (bitwise-repeatable).
  * dk and dv are 0 from lengths[b] on.  Workspace of the size the query names
- * (0 for invalid arguments), 256-byte aligned; other errors as above. */
+ * (0 for invalid arguments), 256-byte aligned; calls that share one must not
+ * overlap; other errors as above. */
 size_t hcmix_grouped_attention_backward_workspace_bytes(int64_t batch, int64_t n_q, int64_t n_k,
                                                         int32_t q_heads, int32_t kv_heads,
                                                         int32_t head_dim);
@@ -644,8 +645,8 @@ hcmix_status hcmix_grouped_attention_backward(
  * and values exact.  A query before the first token gets 0.  lengths: int32
  * [batch], taken within 0 .. capacity.  max_length (1 .. capacity) says how long
  * sequences are expected to be: long ones are split over the chip by it (joined
- * through the workspace of hcmix_kv_cache_attention_workspace_bytes, possibly 0),
- * and longer ones than it are still right.
+ * through the workspace of hcmix_kv_cache_attention_workspace_bytes, possibly 0;
+ * calls that share one must not overlap), and longer ones than it are still right.
  *
  * All of positions, counts, first and lengths are device memory, so that a
  * captured graph can be replayed with other values in them.

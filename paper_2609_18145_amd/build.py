@@ -54,7 +54,7 @@ def _build_marshal() -> None:
     incs = [*include_paths(), sysconfig.get_paths()["include"]]
     cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
-           *[a for p in incs for a in ("-isystem", p)],
+           "-I", os.path.join(ROOT, "include"), *[a for p in incs for a in ("-isystem", p)],
            os.path.join(PKG, "csrc", "marshal.cpp"), "-o", tmp,
            *["-L" + p for p in library_paths()], "-ltorch_python", "-ltorch_cpu", "-lc10"]
     res = subprocess.run(cmd, capture_output=True, text=True)

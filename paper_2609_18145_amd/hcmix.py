@@ -952,11 +952,40 @@ def linear_backward(x, w, dy, dx=None, dw=None, with_dx=True, with_dw=True, accu
 # ---- attention layers past the fixed windows ----
 
 _ROTARY_LAYOUTS = {"half": 0, "pairs": 1}
+_fns = {}
+
+
+def _fn(name):
+    """A library function's address, for the calls in native code."""
+    f = _fns.get(name)
+    if f is None:
+        f = _fns[name] = ctypes.cast(getattr(load(), name), ctypes.c_void_p).value
+    return f
+
+
+def _quick(t):
+    """The current stream where a call can go through the native extension (a
+    plain tensor on the current GPU), else None."""
+    if type(t) is not torch.Tensor or not t.is_cuda:
+        return None
+    i = t.get_device()
+    if i != torch._C._cuda_getDevice():
+        return None
+    if _marshal is None:
+        _native()
+    return torch._C._cuda_getCurrentRawStream(i)
+
+
+def _done(r, what):
+    """What a native call gave: its results, or the status it ends with."""
+    if type(r) is int:
+        raise HcmixError(r, what)
+    return r
 
 
 def _call(dev, what, *args):
-    """A library call on dev's current stream, with dev the current device (a
-    kernel is launched on the current device's behalf)."""
+    """A library call from operands checked here, on dev's current stream, with dev
+    the current device (a kernel is launched on the current device's behalf)."""
     fn = getattr(_lib or load(), what)
     if dev.index == torch._C._cuda_getDevice():
         rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
@@ -1039,6 +1068,12 @@ def rotary(x, freqs, positions=None, layout="half", inverse=False, scale=1.0, ou
     in every sequence.  layout: pairs (j, j + rot / 2) ("half") or (2j, 2j + 1)
     ("pairs").  inverse: by the opposite angle, the backward.  out: x itself (in
     place), or a tensor that shares nothing with it."""
+    st = _quick(x)
+    if st is not None and layout in _ROTARY_LAYOUTS:
+        r = _marshal.rotary(_fn("hcmix_rotary"), x, freqs, positions, _ROTARY_LAYOUTS[layout],
+                            int(bool(inverse)), scale, out, st)
+        if r is not None:
+            return _done(r, "hcmix_rotary")
     if not isinstance(x, torch.Tensor) or x.dim() != 4:
         raise ValueError("x: expected a [batch, n, heads, head_dim] tensor")
     if layout not in _ROTARY_LAYOUTS:
@@ -1083,6 +1118,12 @@ def grouped_attention_forward(q, k, v, causal=True, lengths=None, scale=None, ou
     sees keys up to i + n_k - n_q.  scale defaults to hd ** -0.5.  Returns (out
     bf16 like q, contiguous; lse fp32 [batch, q_heads, n_q]); a row that sees
     nothing gives 0 and -inf."""
+    st = _quick(q)
+    if st is not None:
+        r = _marshal.grouped_forward(_fn("hcmix_grouped_attention_forward"), q, k, v,
+                                     int(bool(causal)), lengths, scale, out, lse, st)
+        if r is not None:
+            return _done(r, "hcmix_grouped_attention_forward")
     dev, dims, operands = _grouped_operands(q, k, v, lengths)
     batch, n_q, _, q_heads, _, hd = dims
     if out is None:
@@ -1102,6 +1143,14 @@ def grouped_attention_backward(q, k, v, out, lse, dout, causal=True, lengths=Non
                                dq=None, dk=None, dv=None, workspace=None):
     """(dq, dk, dv) of ``grouped_attention_forward`` given its results and dout =
     dL/dout (contiguous).  dq, dk, dv may be slices of one packed buffer."""
+    st = _quick(q) if workspace is None else None
+    if st is not None:
+        r = _marshal.grouped_backward(
+            _fn("hcmix_grouped_attention_backward"),
+            _fn("hcmix_grouped_attention_backward_workspace_bytes"), q, k, v, out, lse, dout,
+            int(bool(causal)), lengths, scale, dq, dk, dv, st)
+        if r is not None:
+            return _done(r, "hcmix_grouped_attention_backward")
     dev, dims, operands = _grouped_operands(q, k, v, lengths)
     batch, n_q, n_k, q_heads, kv_heads, hd = dims
     bf, q_shape, kv_shape = torch.bfloat16, (batch, n_q, q_heads, hd), (batch, n_k, kv_heads, hd)
@@ -1152,6 +1201,12 @@ def kv_cache_append(k, v, positions, cache, capacity, counts=None):
     positions[b] and behind (int32 [batch] on the GPU), the first counts[b] of every
     sequence where counts is given.  What was held from positions[b] on is
     dropped; tokens at `capacity` and behind are left out."""
+    st = _quick(k)
+    if st is not None:
+        r = _marshal.cache_append(_fn("hcmix_kv_cache_append"), k, v, positions, counts, cache,
+                                  capacity, st)
+        if r is not None:
+            return _done(r, "hcmix_kv_cache_append")
     if not isinstance(k, torch.Tensor) or k.dim() != 4:
         raise ValueError("k: expected a [batch, tokens, kv_heads, head_dim] tensor")
     p_k = _heads(k, "k", _ANY, torch.bfloat16)
@@ -1171,6 +1226,12 @@ def kv_cache_append(k, v, positions, cache, capacity, counts=None):
 def kv_cache_read(cache, capacity, kv_heads, head_dim, first, lengths, tokens, k=None, v=None):
     """(k, v) bf16 [batch, tokens, kv_heads, head_dim]: the values held for tokens
     first[b] and behind, 0 outside 0 .. lengths[b] - 1 (int32 [batch] on the GPU)."""
+    st = _quick(first)
+    if st is not None:
+        r = _marshal.cache_read(_fn("hcmix_kv_cache_read"), first, lengths, cache, capacity,
+                                kv_heads, head_dim, tokens, k, v, st)
+        if r is not None:
+            return _done(r, "hcmix_kv_cache_read")
     if not isinstance(first, torch.Tensor) or first.dim() != 1:
         raise ValueError("first: expected a [batch] tensor")
     batch, dev = first.shape[0], first.device
@@ -1194,6 +1255,13 @@ def kv_cache_attention(q, lengths, cache, capacity, kv_heads, scale=None, max_le
     token standing at lengths[b] - 1 (int32 [batch] on the GPU, the new tokens
     included): every token sees those up to itself.  scale defaults to hd ** -0.5;
     max_length: how long sequences are expected to be (default: capacity)."""
+    st = _quick(q) if workspace is None else None
+    if st is not None:
+        r = _marshal.cache_attention(
+            _fn("hcmix_kv_cache_attention"), _fn("hcmix_kv_cache_attention_workspace_bytes"), q,
+            lengths, cache, capacity, kv_heads, scale, max_length, out, st)
+        if r is not None:
+            return _done(r, "hcmix_kv_cache_attention")
     if not isinstance(q, torch.Tensor) or q.dim() != 4:
         raise ValueError("q: expected a [batch, tokens, q_heads, head_dim] tensor")
     p_q = _heads(q, "q", _ANY, torch.bfloat16)

@@ -264,3 +264,55 @@ def test_a_cache_that_the_library_has_no_kernel_for():
 def test_hybrid_decoder_is_causal_only(untouched):
     h = HybridStack([0, 1], [z(64, 64)] * 2, [z(64, 64)] * 2, [], 1, causal=False)
     refused(h.decoder, 2, 16, "cpu", match="causal")
+
+
+def test_native_calls_leave_other_operands_to_the_binding():
+    """Operands off the GPU, of other types or too few: None, and no error left behind."""
+    m = hcmix._native()
+    q, pos, c = z(2, 3, 2, 64), z(2, dtype=i32), z(1024, dtype=torch.uint8)
+    f = z(32, dtype=f64)
+    for call, args in ((m.rotary, (1, q, f, None, 0, 0, 1.0, None, 0)), (m.rotary, (1,)),
+                       (m.grouped_forward, (1, q, q, q, 1, None, None, None, None, 0)),
+                       (m.grouped_forward, (1, None, q, q, 1, None, None, None, None, 0)),
+                       (m.grouped_backward, (1, 1, q, q, q, q, q, q, 1, None, None, None, None, None, 0)),
+                       (m.cache_append, (1, q, q, pos, None, c, 10, 0)), (m.cache_append, ()),
+                       (m.cache_read, (1, pos, pos, c, 10, 2, 64, 3, None, None, 0)),
+                       (m.cache_attention, (1, 1, q, pos, c, 10, 2, None, None, None, 0)),
+                       (m.heads, (q, (None,) * 4, bf, None)), (m.heads, ([1], (None,) * 4, bf, None))):
+        assert call(*args) is None
+
+
+@pytest.mark.gpu
+def test_refusals_on_the_gpu_say_what_is_wrong():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    g = lambda *a, **k: z(*a, **k).cuda()  # noqa: E731
+    q, k, f, pos = g(2, 5, 4, 64), g(2, 7, 2, 64), g(32, dtype=f64), g(2, dtype=i32)
+    out, lse = g(2, 5, 4, 64), g(2, 4, 5, dtype=f32)
+    cache = hcmix.alloc_kv_cache(2, 10, 2, 64, "cuda")
+    for fn, args, kw, match in (
+            (hcmix.rotary, (q, g(32, dtype=f32)), {}, "freqs"),
+            (hcmix.rotary, (q, f.cpu()), {}, "freqs"),
+            (hcmix.rotary, (q, f), dict(positions=g(2, 4, dtype=i32)), "positions"),
+            (hcmix.rotary, (q, f), dict(out=g(2, 5, 3, 64)), "out"),
+            (hcmix.rotary, (q, f), dict(layout="x"), "layout"),
+            (hcmix.grouped_attention_forward, (q, k, g(2, 6, 2, 64)), {}, "v"),
+            (hcmix.grouped_attention_forward, (q, k.cpu(), k), {}, "k"),
+            (hcmix.grouped_attention_forward, (q, k, k), dict(lengths=g(3, dtype=i32)), "lengths"),
+            (hcmix.grouped_attention_forward, (q, k, k), dict(out=out[:, :, ::2]), "out"),
+            (hcmix.grouped_attention_backward, (q, k, k, out, lse, g(2, 5, 4, 64, dtype=f32)), {}, "dout"),
+            (hcmix.grouped_attention_backward, (q, k, k, out, lse, out), dict(dv=g(2, 7, 4, 64)), "dv"),
+            (hcmix.kv_cache_append, (k, k, g(3, dtype=i32), cache, 10), {}, "positions"),
+            (hcmix.kv_cache_append, (k, k, pos, cache.cpu(), 10), {}, "cache"),
+            (hcmix.kv_cache_read, (cache, 10, 2, 64, pos, pos.cpu(), 3), {}, "lengths"),
+            (hcmix.kv_cache_attention, (q, g(2, dtype=torch.int64), cache, 10, 2), {}, "lengths")):
+        refused(fn, *args, match=match, **kw)
+    for fn, args, kw in ((hcmix.grouped_attention_forward, (g(2, 5, 3, 64), k, k), {}),   # 3 heads over 2
+                         (hcmix.grouped_attention_forward, (g(2, 5, 2, 32),) * 3, {}),
+                         (hcmix.grouped_attention_backward, (q, k, k, out, lse, out), dict(scale=0.0)),
+                         (hcmix.kv_cache_append, (k, k, pos, cache, 1000), {}),           # a short cache
+                         (hcmix.kv_cache_attention, (q, pos, cache, 10, 3), {}),
+                         (hcmix.rotary, (q, f), dict(scale=float("nan")))):
+        with pytest.raises(hcmix.HcmixError):
+            fn(*args, **kw)
+    torch.cuda.synchronize()
