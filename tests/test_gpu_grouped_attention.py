@@ -201,3 +201,33 @@ def test_on_another_stream_and_captured():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_autograd_captured_whole():
+    """Rotary and attention with their gradients in one captured graph, replayed on
+    other inputs between eager runs of the same: as those."""
+    g = torch.Generator().manual_seed(7)
+    freqs, _ = hcmix.rotary_frequencies(64)
+
+    def step(q, k, v, do):
+        q, k, v = (t.detach().requires_grad_(True) for t in (q, k, v))
+        out = hcmix.GroupedAttention.apply(hcmix.Rotary.apply(q, freqs), hcmix.Rotary.apply(k, freqs), v)
+        return (out.detach(), *torch.autograd.grad(out, (q, k, v), do))
+    sets = [[torch.randn((2, 90, h, 64), generator=g).to(torch.bfloat16).cuda() for h in (4, 2, 2, 4)]
+            for _ in range(3)]
+    ops = [t.clone() for t in sets[0]]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*ops)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(*ops)
+    for other in sets:
+        for a, b in zip(ops, other):
+            a.copy_(b)
+        graph.replay()
+        want = step(*other)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -196,3 +196,27 @@ def test_packed_queries_other_scale_and_graph():
         want = step(caches[1])
         torch.cuda.synchronize()
         assert torch.equal(out, want), p
+
+
+def test_calls_on_two_streams_at_once():
+    """Two batches decoded on streams of their own, each with its cache: as one
+    after the other."""
+    def decode(seed):
+        g = torch.Generator().manual_seed(seed)
+        cache = hcmix.alloc_kv_cache(4, 700, 2, 64, "cuda")
+        outs = []
+        k, v = (torch.randn((4, 600, 2, 64), generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+        hcmix.kv_cache_append(k, v, ints([0] * 4), cache, 700)
+        for p in range(600, 620):
+            q = torch.randn((4, 1, 8, 64), generator=g).to(torch.bfloat16).cuda()
+            hcmix.kv_cache_append(q[:, :, :2], q[:, :, 2:4], ints([p] * 4), cache, 700)
+            outs.append(hcmix.kv_cache_attention(q, ints([p + 1] * 4), cache, 700, 2))
+        return torch.stack(outs)
+    want = [decode(s) for s in (1, 2)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for i, st in enumerate(streams):
+        with torch.cuda.stream(st):
+            got.append(decode(i + 1))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
