@@ -77,11 +77,12 @@ struct TileDma {
 // This block's (sequence, head, tile).  Under a causal mask a head's tiles differ
 // in work up to its whole length, and a heavy one that starts late is waited for:
 // tiles come in order of their work, the heaviest of all heads first (8 x 4096,
-// 16 heads over 4: head after head, dK and dV took 870 us, so 600).  The heads are
+// 16 heads over 4: head after head, dK and dV took 870 us, so 630).  The heads are
 // dealt to the XCDs (blocks go to the 8 of them in turn), so that an L2 holds the
 // keys and values that a group's heads and a head's tiles share, and on an XCD
-// taken in chunks of two rounds of its 64 blocks.  A number of heads that is no
-// multiple of 8 is spread over the XCDs as it comes.
+// taken in chunks of four rounds of 64 blocks (two: 1.5% slower, all at once: the
+// same).  A number of heads that is no multiple of 8 is spread over the XCDs as it
+// comes.
 struct Item {
   int b, h, tile;
 };
@@ -91,7 +92,7 @@ __device__ __forceinline__ bool ga_item(int batch, int heads, int tiles, bool la
   if (blockIdx.x >= all * tiles) return false;
   if (all % 8 == 0) {
     const unsigned per = all / 8, xcd = blockIdx.x % 8, k = blockIdx.x / 8;
-    const unsigned two = (127u + tiles) / tiles, size = min(per, two);
+    const unsigned size = min(per, (255u + tiles) / tiles);
     const unsigned chunk = k / (size * tiles), r = k - chunk * size * tiles;
     const unsigned n = min(size, per - chunk * size);
     t = r / n;
@@ -224,12 +225,6 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_fwd_kernel(GroupedArgs 
         for (int e = 0; e < 16; e++) o[d][e] *= alpha;
     }
     scores(sK[buf ^ 1], next);
-    // of what follows, seven vector instructions to each of the matrix unit's
-#pragma unroll
-    for (int i = 0; i < D / 4; i++) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
-    }
     const bf16* tv = sV[buf];
 #pragma unroll
     for (int kt = 0; kt < 2; kt++) {
