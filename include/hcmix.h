@@ -579,15 +579,17 @@ hcmix_status hcmix_rotary(int64_t rows, int32_t heads, int32_t head_dim, int32_t
  * Query i sees key j when j < lengths[b] (int32 [batch], taken within 0 .. n_k;
  * NULL: n_k) and, causal != 0, j <= i + n_k - n_q (the last query stands at the
  * last key).  A row that sees nothing gets out = 0 and lse = -inf, and gives no
- * gradient.  What keys and values from lengths[b] on hold is never taken.
+ * gradient.  What keys and values from lengths[b] on hold is never taken; those
+ * before it have to be finite also where the causal mask hides them (a weight of 0
+ * meets them).
  *   q, k, v: bf16 as above, head_dim 64 or 128; out: bf16 [batch][n_q][q_heads]
  *   [head_dim], lse: fp32 [batch][q_heads][n_q], both contiguous.
  * Precision: products of bf16 with fp32 accumulation, softmax statistics in fp32,
  * P (and the backward's P and dS) rounded to bf16 for the second products.
- * n_q, n_k <= 2^20, q_heads <= 1024, batch * n <= 2^30; scale positive, finite.
+ * n_q, n_k <= 2^20, q_heads <= 1024, batch * n <= 2^30; scale 2^-24 .. 2^24.
  * HCMIX_ERR_INVALID_VALUE: null pointers (lengths may be), sizes < 1 or past
- * those bounds, q_heads no multiple of kv_heads, causal not 0 or 1, a scale that
- * is not positive and finite, strides outside those bounds, overlaps.
+ * those bounds, q_heads no multiple of kv_heads, causal not 0 or 1, strides
+ * outside theirs, overlaps.
  * HCMIX_ERR_UNSUPPORTED: another head_dim, strides that are no multiple of 8,
  * bf16 pointers not 16-byte, others not 4-byte aligned. */
 hcmix_status hcmix_grouped_attention_forward(
@@ -652,8 +654,8 @@ hcmix_status hcmix_grouped_attention_backward(
  * captured graph can be replayed with other values in them.
  * HCMIX_ERR_INVALID_VALUE: null pointers (counts may be), sizes < 1, batch above
  * 65535, capacity above 2^24, tokens above 2^16, heads above 1024, q_heads no
- * multiple of kv_heads, a cache shorter than the query, a scale that is not
- * positive and finite, strides outside those bounds, overlaps.
+ * multiple of kv_heads, a cache shorter than the query, a scale outside 2^-24 ..
+ * 2^24, strides outside their bounds, overlaps.
  * HCMIX_ERR_UNSUPPORTED: head_dim not 64 or 128, strides that are no multiple of
  * 8, bf16 pointers not 16-byte, the cache and workspace not 256-byte, others not
  * 4-byte aligned. */

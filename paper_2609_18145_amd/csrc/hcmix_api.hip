@@ -1467,7 +1467,8 @@ Rows rows_of(const void* p, int64_t rows, int64_t stride, int64_t width, size_t 
 
 constexpr int64_t kMaxStride = (int64_t)1 << 24;     // elements between two positions
 
-bool positive(float v) { return v > 0.f && v <= 3.4028235e38f; }
+// An attention's scale: by 2^-24 and 2^24 its statistics stay in 32 bits.
+bool scale_ok(float v) { return v >= 0x1p-24f && v <= 0x1p24f; }
 
 // Head counts and strides of bf16 [..][heads][head_dim] operands.
 hcmix_status check_heads(int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
@@ -1543,7 +1544,7 @@ hcmix_status hcmix_grouped_attention_forward(
   if (!q || !k || !v || !out || !lse) return HCMIX_ERR_INVALID_VALUE;
   hcmix_status st = check_grouped(batch, n_q, n_k, q_heads, kv_heads, head_dim);
   if (st != HCMIX_OK) return st;
-  if ((causal != 0 && causal != 1) || !positive(scale)) return HCMIX_ERR_INVALID_VALUE;
+  if ((causal != 0 && causal != 1) || !scale_ok(scale)) return HCMIX_ERR_INVALID_VALUE;
   const int64_t qw = (int64_t)q_heads * head_dim, kw = (int64_t)kv_heads * head_dim;
   if ((st = check_stride(q_stride, qw)) != HCMIX_OK || (st = check_stride(k_stride, kw)) != HCMIX_OK ||
       (st = check_stride(v_stride, kw)) != HCMIX_OK)
@@ -1599,7 +1600,7 @@ hcmix_status hcmix_grouped_attention_backward(
     return HCMIX_ERR_INVALID_VALUE;
   hcmix_status st = check_grouped(batch, n_q, n_k, q_heads, kv_heads, head_dim);
   if (st != HCMIX_OK) return st;
-  if ((causal != 0 && causal != 1) || !positive(scale)) return HCMIX_ERR_INVALID_VALUE;
+  if ((causal != 0 && causal != 1) || !scale_ok(scale)) return HCMIX_ERR_INVALID_VALUE;
   const size_t need = grouped_workspace_bytes(batch, n_q, n_k, q_heads, kv_heads, head_dim);
   if (workspace_bytes < need) return HCMIX_ERR_INVALID_VALUE;
   const int64_t qw = (int64_t)q_heads * head_dim, kw = (int64_t)kv_heads * head_dim;
@@ -1791,7 +1792,7 @@ hcmix_status hcmix_kv_cache_attention(int64_t batch, int64_t capacity, int32_t q
   hcmix_status st = check_kv_call(batch, capacity, kv_heads, head_dim, tokens, cache, cache_bytes);
   if (st != HCMIX_OK) return st;
   if ((st = check_heads(q_heads, kv_heads, head_dim)) != HCMIX_OK) return st;
-  if (!positive(scale) || max_length < 1 || max_length > capacity) return HCMIX_ERR_INVALID_VALUE;
+  if (!scale_ok(scale) || max_length < 1 || max_length > capacity) return HCMIX_ERR_INVALID_VALUE;
   const int64_t qw = (int64_t)q_heads * head_dim, rows = batch * tokens;
   if ((st = check_stride(q_stride, qw)) != HCMIX_OK) return st;
   const KvParts p = kv_parts(batch, capacity, kv_heads, head_dim);

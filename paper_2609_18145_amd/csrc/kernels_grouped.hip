@@ -484,6 +484,7 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_q_kernel(GroupedArg
 // the query tiles that see them of the group's heads one after the other.  Where
 // the key tiles are too few for the chip, a.parts blocks share that sequence of
 // query tiles and leave fp32 sums, which ga_join_kernel adds in order.
+//
 // A lane's 16 rows have statistics of their own, read from LDS: S and dP start from
 // them instead of 0, which saves the vector unit its subtractions (8 x 4096, 16
 // heads of 64 over 4: 980 us for the whole backward, 1008 without).  KS as in the
@@ -745,7 +746,7 @@ template <int D>
 hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
   const int64_t kv = ga_tiles(a.n_k) * a.kv_heads * a.parts, q = ga_tiles(a.n_q) * a.q_heads;
   const int64_t per = std::max(kv, q);
-  // (parts > 1 has few blocks, hence one slice: the sums' places depend on the batch)
+  // (every slice's sums lie at the workspace's start, in its own extents)
   const int64_t most = GA_MAX_BLOCKS / per > 0 ? GA_MAX_BLOCKS / per : 1;
   for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
     const int64_t nb = a.batch - b0 < most ? a.batch - b0 : most;

@@ -53,7 +53,8 @@ SHARED = [
     (dict(batch=1 << 28), INVALID), (dict(heads=5), INVALID), (dict(kv=0), INVALID),
     (dict(heads=0), INVALID), (dict(heads=2048, qs=1 << 20), INVALID), (dict(causal=2), INVALID),
     (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=NAN), INVALID),
-    (dict(scale=INF), INVALID), (dict(q=None), INVALID), (dict(k=None), INVALID),
+    (dict(scale=INF), INVALID), (dict(scale=2.0 ** -25), INVALID), (dict(scale=2.0 ** 25), INVALID),
+    (dict(q=None), INVALID), (dict(k=None), INVALID),
     (dict(v=None), INVALID), (dict(out=None), INVALID), (dict(lse=None), INVALID),
     (dict(qs=248), INVALID), (dict(ks=120), INVALID), (dict(vs=0), INVALID),
     (dict(qs=(1 << 32) + 8), INVALID), (dict(hd=96), UNSUPPORTED), (dict(hd=256), UNSUPPORTED),
