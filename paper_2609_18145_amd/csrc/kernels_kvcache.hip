@@ -213,13 +213,63 @@ __global__ __launch_bounds__(KV_THREADS) void kv_append_kernel(KvAppendArgs a) {
   }
 }
 
+// One token of every sequence, the decoding step's form: a wave to a head, lane l
+// the dimensions l and, for 128, 64 + l.  (64 sequences of 8 heads of 64: 6.5 us with
+// the kernel above, whose 256 threads meet twice for one row, 3.4 so.)
+template <int D>
+__global__ __launch_bounds__(KV_THREADS) void kv_append_one_kernel(KvAppendArgs a) {
+  constexpr int DL = D / 64;
+  const int lane = threadIdx.x & 63, b = blockIdx.y;
+  const int h = blockIdx.x * KV_WAVES + wave_index<KV_WAVES>();
+  if (h >= a.kv_heads) return;
+  const int pos = __builtin_amdgcn_readfirstlane(a.positions[b]);
+  const int count = a.counts ? __builtin_amdgcn_readfirstlane(a.counts[b]) : 1;
+  if (pos < 0 || pos >= a.capacity || count < 1) return;
+  const int old = pos % KB;
+  const size_t at = ((size_t)b * a.kv_heads + h) * a.blocks + pos / KB;
+  unsigned char *ck = a.keys + at * KB * D, *cv = a.values + at * KB * D;
+  float* scales = a.scales + 2 * at;
+  const float2 held = old ? *(const float2*)scales : float2{0.f, 0.f};
+  float x[DL], y[DL], mk = 0.f, mv = 0.f;
+#pragma unroll
+  for (int i = 0; i < DL; i++) {
+    x[i] = (float)a.k[(size_t)b * a.k_stride + (size_t)h * D + 64 * i + lane];
+    y[i] = (float)a.v[(size_t)b * a.v_stride + (size_t)h * D + 64 * i + lane];
+    mk = fmaxf(mk, fabsf(x[i]));
+    mv = fmaxf(mv, fabsf(y[i]));
+  }
+#pragma unroll
+  for (int s = 32; s; s >>= 1) {
+    mk = fmaxf(mk, __shfl_xor(mk, s));
+    mv = fmaxf(mv, __shfl_xor(mv, s));
+  }
+  const float sk = fmaxf(kv_scale(mk), held.x), sv = fmaxf(kv_scale(mv), held.y);
+  if (lane == 0) *(float2*)scales = float2{sk, sv};
+  if (old && sk > held.x)
+    for (int i = lane; i < old * (D / 16); i += 64)
+      ((u32x4*)ck)[i] = kv_rescaled(((u32x4*)ck)[i], held.x / sk);
+  if (old && sv > held.y) {
+    for (int i = lane; i < KB * D / 16; i += 64)
+      ((u32x4*)cv)[i] = kv_rescaled(((u32x4*)cv)[i], held.y / sv);
+    // the new byte goes between them: this wave's stores stay in order
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
+#pragma unroll
+  for (int i = 0; i < DL; i++) {
+    ck[old * D + 64 * i + lane] = kv_byte(x[i] * (1.f / sk));
+    cv[(64 * i + lane) * KB + kv_slot(old)] = kv_byte(y[i] * (1.f / sv));
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Read: tokens first[b] .. + tokens of every sequence, zeros from lengths[b] on;
 // a block of threads per touched block, as the append has them.
 // ---------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(KV_THREADS) void kv_read_kernel(KvReadArgs a) {
-  constexpr int DV = D / 8, ITEMS = KB / 4 * DV;
+  // an item is R tokens x 8 dimensions: one to a thread
+  constexpr int DV = D / 8, R = D / 32;
+  static_assert(KB / R * DV == KV_THREADS, "");
   __shared__ unsigned tile[D * KV_ROW];
   const int h = blockIdx.y, b = blockIdx.z;
   const int from = a.first[b], len = kv_bounded(a.lengths[b], 0, a.capacity);
@@ -228,37 +278,45 @@ __global__ __launch_bounds__(KV_THREADS) void kv_read_kernel(KvReadArgs a) {
   const bool held = start >= 0 && start < len;     // (then a block of the cache)
   const size_t at = held ? ((size_t)b * a.kv_heads + h) * a.blocks + start / KB : 0;
   const unsigned char *ck = a.keys + at * KB * D, *cv = a.values + at * KB * D;
-  if (held)
-    for (int i = threadIdx.x; i < D * (KB / 16); i += KV_THREADS) {
-      const u32x4 v = ((const u32x4*)cv)[i];
-      unsigned* w = tile + i / (KB / 16) * KV_ROW + i % (KB / 16) * 4;
+  const int g = threadIdx.x / DV, p = threadIdx.x % DV;
+  uint2 c[R];
+  float2 scale = {0.f, 0.f};
+  if (held) {
+    constexpr int PER = D * (KB / 16) / KV_THREADS;
+    u32x4 v[PER];
 #pragma unroll
-      for (int e = 0; e < 4; e++) w[e] = v[e];
+    for (int i = 0; i < PER; i++) v[i] = ((const u32x4*)cv)[threadIdx.x + KV_THREADS * i];
+#pragma unroll
+    for (int r = 0; r < R; r++) c[r] = *(const uint2*)(ck + (R * g + r) * D + 8 * p);
+    scale = *(const float2*)(a.scales + 2 * at);
+#pragma unroll
+    for (int i = 0; i < PER; i++) {
+      const int n = threadIdx.x + KV_THREADS * i;
+      unsigned* w = tile + n / (KB / 16) * KV_ROW + n % (KB / 16) * 4;
+#pragma unroll
+      for (int e = 0; e < 4; e++) w[e] = v[i][e];
     }
-  const float sk = held ? a.scales[2 * at] : 0.f, sv = held ? a.scales[2 * at + 1] : 0.f;
+  }
   __syncthreads();
-  for (int item = threadIdx.x; item < ITEMS; item += KV_THREADS) {
-    const int g = item / DV, p = item % DV;
-    unsigned w[8];
+  unsigned w[8];
 #pragma unroll
-    for (int e = 0; e < 8; e++) w[e] = held ? tile[kv_word(8 * p + e, g)] : 0;
+  for (int e = 0; e < 8; e++) w[e] = held ? tile[kv_word(8 * p + e, R * g / 4)] : 0;
 #pragma unroll
-    for (int r = 0; r < 4; r++) {
-      const int64_t pos = start + 4 * g + r, t = pos - from;
-      if (t < 0 || t >= a.tokens) continue;
-      bf16x8 x = {}, y = {};
-      if (held && pos < len) {
-        const uint2 c = *(const uint2*)(ck + (size_t)(4 * g + r) * D + 8 * p);
+  for (int r = 0; r < R; r++) {
+    const int64_t pos = start + R * g + r, t = pos - from;
+    if (t < 0 || t >= a.tokens) continue;
+    bf16x8 x = {}, y = {};
+    if (held && pos < len) {
+      const int byte = 8 * ((R * g + r) & 3);      // of its group of four tokens
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-          x[e] = to_bf16(kv_value(((e < 4 ? c.x : c.y) >> (8 * (e & 3))) & 255) * sk);
-          y[e] = to_bf16(kv_value((w[e] >> (8 * r)) & 255) * sv);
-        }
+      for (int e = 0; e < 8; e++) {
+        x[e] = to_bf16(kv_value(((e < 4 ? c[r].x : c[r].y) >> (8 * (e & 3))) & 255) * scale.x);
+        y[e] = to_bf16(kv_value((w[e] >> byte) & 255) * scale.y);
       }
-      const size_t o = (((size_t)b * a.tokens + t) * a.kv_heads + h) * D + 8 * p;
-      *(bf16x8*)(a.k + o) = x;
-      *(bf16x8*)(a.v + o) = y;
     }
+    const size_t o = (((size_t)b * a.tokens + t) * a.kv_heads + h) * D + 8 * p;
+    *(bf16x8*)(a.k + o) = x;
+    *(bf16x8*)(a.v + o) = y;
   }
 }
 
@@ -500,6 +558,12 @@ hipError_t kv_attention_launch(const KvAttentionArgs& a, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st) {
+  if (a.tokens == 1) {
+    const dim3 grid((a.kv_heads + KV_WAVES - 1) / KV_WAVES, a.batch);
+    if (a.head_dim == 64) kv_append_one_kernel<64><<<grid, KV_THREADS, 0, st>>>(a);
+    else kv_append_one_kernel<128><<<grid, KV_THREADS, 0, st>>>(a);
+    return hipGetLastError();
+  }
   const dim3 grid((a.tokens + KB - 2) / KB + 1, a.kv_heads, a.batch);
   if (a.head_dim == 64) kv_append_kernel<64><<<grid, KV_THREADS, 0, st>>>(a);
   else kv_append_kernel<128><<<grid, KV_THREADS, 0, st>>>(a);

@@ -64,8 +64,10 @@ def test_cache(launches, batch, capacity, kv, tokens):  # noqa: F811
     dims = i64(batch, capacity) + i32(kv, 64) + i64(tokens)
     (x, y, z), _, _ = launches("hcmix_kv_cache_append", dims + [ptr(0)] + i64(kv * 64) + [ptr(1)]
                                + i64(kv * 64) + [ptr(2), NONE, ptr(3), size, NONE])[0]
-    # from the last token of a block on
-    assert (y, z) == (kv, batch) and 64 * x >= tokens + 63 - 63 // 64 and 64 * (x - 1) < tokens + 63
+    if tokens == 1:       # a wave to a head
+        assert 4 * x >= kv > 4 * (x - 1) and (y, z) == (batch, 1)
+    else:                 # blocks from the last token of one on
+        assert (y, z) == (kv, batch) and 64 * x >= tokens + 63 > 64 * (x - 1)
     (x, y, z), _, _ = launches("hcmix_kv_cache_read", dims + [ptr(0), ptr(1), ptr(3), size, ptr(4),
                                                               ptr(5), NONE])[0]
     assert (y, z) == (kv, batch) and 64 * x >= tokens
