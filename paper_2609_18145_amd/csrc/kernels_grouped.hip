@@ -24,8 +24,7 @@ namespace {
 
 constexpr int GA_THREADS = 256;
 constexpr float GA_LOG2E = 1.4426950408889634f, GA_LN2 = 0.6931471805599453f;
-constexpr int GA_TILE = 64;         // rows of an LDS tile
-// Rows of a block (32 to a wave).
+// Rows of a block of four waves (32 to a wave).
 constexpr int GA_ROWS = 128;
 
 // A buffer's index known at compile time: its LDS addresses are then offsets in
@@ -45,15 +44,15 @@ __device__ __forceinline__ bf16x8 ga_trfrag(const bf16* t, int k0, int c0, int l
 
 // A tile's way straight into LDS: rows row0 .. + R of an array with rows `stride`
 // elements apart; rows at `valid` and behind are copies of the last before it
-// (finite where the valid ones are: their P is 0).  A wave copies every fourth
-// piece of 8 rows by 64 columns, lane l the 16 bytes that the swizzle wants there.
-template <int D, int R>
+// (finite where the valid ones are: their P is 0).  A wave copies every W-th piece
+// of 8 rows by 64 columns, lane l the 16 bytes that the swizzle wants there.
+template <int D, int R, int W = 4>
 struct TileDma {
-  static constexpr int PER = D / 64 * R / 32;        // pieces of a wave
+  static constexpr int PER = D / 64 * R / 8 / W;     // pieces of a wave
   unsigned off[PER];                                 // source bytes from row row0
   int wave, lane;
   __device__ __forceinline__ unsigned at(int j, int last, unsigned stride) const {
-    const int blk = wave + 4 * j, r = blk % (R / 8) * 8 + (lane >> 3);
+    const int blk = wave + W * j, r = blk % (R / 8) * 8 + (lane >> 3);
     return 2 * ((unsigned)min(r, last) * stride + blk / (R / 8) * HD + 8 * ((lane & 7) ^ att_sw(r)));
   }
   __device__ __forceinline__ TileDma(int w, int l, int64_t stride) : wave(w), lane(l) {
@@ -65,11 +64,11 @@ struct TileDma {
     const bf16* src = uniform_base(base + (size_t)row0 * stride);
     if (row0 + R <= valid) {
 #pragma unroll
-      for (int j = 0; j < PER; j++) dma16_at(src, off[j], tile + (wave + 4 * j) * 512);
+      for (int j = 0; j < PER; j++) dma16_at(src, off[j], tile + (wave + W * j) * 512);
     } else {
 #pragma unroll
       for (int j = 0; j < PER; j++)
-        dma16_at(src, at(j, valid - 1 - row0, (unsigned)stride), tile + (wave + 4 * j) * 512);
+        dma16_at(src, at(j, valid - 1 - row0, (unsigned)stride), tile + (wave + W * j) * 512);
     }
   }
 };
@@ -141,76 +140,80 @@ __device__ __forceinline__ void ga_rows(bf16x8 (&f)[D / 16], const bf16* base, s
 // what has been accumulated, and the exchange of the maximum between the two
 // lanes of a query, is a rare branch.
 //
-// KS = 2: where the blocks are fewer than the CUs, two sets of four waves share a
-// block's key tiles, one the even and one the odd ones, and join at the end (a
-// wave alone on its SIMD waits for itself: 3 x 1000, 8 heads of 128 over 2,
-// ragged: 23.7 us, 20.3 so).
+// A block is W waves of queries by KS sets that share its key tiles in turn and
+// join at the end: 4 by 1, and 2 by 4 where the blocks of 128 queries are no more
+// than the CUs.  Then a wave alone on its SIMD waits for itself, and a block's
+// whole length is the call's time.  us with 4 by 1, 4 by 2 and 2 by 4, causal, 8
+// heads over 2: 3 x 1000 of 128 23.7, 21.0, 22.0; 1 x 1000 of 64 (4 by 2:) 13.3,
+// 10.4; 2 x 2048 of 64 23.8, 20.8; 1 x 4000 of 128 58.1, 52.3; 4 x 64 queries of
+// 2000 keys of 128 30.5, 22.8.
 constexpr float GA_SLACK = 8.f;
 
-template <int D, int KS>
-__global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
-  __shared__ __attribute__((aligned(1024))) bf16 sKV[KS][2][2][GA_TILE * D];   // keys, values
+template <int D, int W, int KS>
+__global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
+  constexpr int ROWS = 32 * W, TILE = KS == 1 ? 64 : 32;       // queries of a block, keys of a tile
+  __shared__ __attribute__((aligned(1024))) bf16 sKV[KS][2][2][TILE * D];   // keys, values
   Item it;
-  if (!ga_item(a.batch, a.q_heads, (a.n_q + GA_ROWS - 1) / GA_ROWS, a.causal, &it)) return;
+  if (!ga_item(a.batch, a.q_heads, (a.n_q + ROWS - 1) / ROWS, a.causal, &it)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = wave_index<GA_THREADS * KS / 64>() & 3, set = wave_index<GA_THREADS * KS / 64>() >> 2;
+  const int wave = wave_index<W * KS>() % W, set = wave_index<W * KS>() / W;
   const int kvh = it.h / a.group, len = ga_length(a, it.b), off = a.n_k - a.n_q;
-  const int blk0 = it.tile * GA_ROWS, q0 = blk0 + 32 * wave;
+  const int blk0 = it.tile * ROWS, q0 = blk0 + 32 * wave;
   const bf16* qb = a.q + (size_t)it.b * a.n_q * a.q_stride + (size_t)it.h * D;
   const bf16* kb = a.k + (size_t)it.b * a.n_k * a.k_stride + (size_t)kvh * D;
   const bf16* vb = a.v + (size_t)it.b * a.n_k * a.v_stride + (size_t)kvh * D;
   // keys that the block's last query, and this wave's, sees; keys that all of its do
-  const int blk_end = a.causal ? min(len, blk0 + GA_ROWS + off) : len;
+  const int blk_end = a.causal ? min(len, blk0 + ROWS + off) : len;
   const int wave_end = a.causal ? min(len, q0 + 32 + off) : len;
   const int full_end = a.causal ? min(len, q0 + 1 + off) : len;
   // tiles of the block, of this set (tile t of it is tile t KS + set), that this wave sees
-  const int all = blk_end > 0 ? (blk_end + GA_TILE - 1) / GA_TILE : 0;
+  const int all = blk_end > 0 ? (blk_end + TILE - 1) / TILE : 0;
   const int turns = (all + KS - 1) / KS, tiles = (all - set + KS - 1) / KS;
-  const int seen = q0 < a.n_q && wave_end > 0 ? (wave_end + GA_TILE - 1) / GA_TILE : 0;
+  const int seen = q0 < a.n_q && wave_end > 0 ? (wave_end + TILE - 1) / TILE : 0;
   const int mine = (seen - set + KS - 1) / KS;
-  bf16(*sK)[GA_TILE * D] = sKV[set][0];
-  bf16(*sV)[GA_TILE * D] = sKV[set][1];
+  bf16(*sK)[TILE * D] = sKV[set][0];
+  bf16(*sV)[TILE * D] = sKV[set][1];
   bf16x8 qf[D / 16];
   ga_rows<D>(qf, qb, a.q_stride, q0, a.n_q, lane);
   f32x16 o[D / 32] = {};
   const float sc = a.scale * GA_LOG2E;
   float m = -3e38f, l = 0.f, limit = -INFINITY;      // limit: the score from which m grows
-  const TileDma<D, GA_TILE> dk(wave, lane, a.k_stride), dv(wave, lane, a.v_stride);
+  const TileDma<D, TILE, W> dk(wave, lane, a.k_stride), dv(wave, lane, a.v_stride);
   auto load_k = [&](int t, bf16* to) {
-    if (t < tiles) dk.load(kb, a.k_stride, (t * KS + set) * GA_TILE, len, to);
+    if (t < tiles) dk.load(kb, a.k_stride, (t * KS + set) * TILE, len, to);
   };
   auto load_v = [&](int t, bf16* to) {
-    if (t < tiles) dv.load(vb, a.v_stride, (t * KS + set) * GA_TILE, len, to);
+    if (t < tiles) dv.load(vb, a.v_stride, (t * KS + set) * TILE, len, to);
   };
-  auto scores = [&](const bf16* tk, f32x16 (&r)[2]) {
+  auto scores = [&](const bf16* tk, f32x16 (&r)[TILE / 32]) {
 #pragma unroll
-    for (int kt = 0; kt < 2; kt++) {
+    for (int kt = 0; kt < TILE / 32; kt++) {
       r[kt] = f32x16{};
 #pragma unroll
       for (int ks = 0; ks < D / 16; ks++)
-        r[kt] = mfma32(ga_frag<GA_TILE>(tk, 32 * kt, 16 * ks, lane), qf[ks], r[kt]);
+        r[kt] = mfma32(ga_frag<TILE>(tk, 32 * kt, 16 * ks, lane), qf[ks], r[kt]);
     }
   };
-  auto turn = [&](auto buf, int t, f32x16 (&s)[2], f32x16 (&next)[2]) {   // buf: t % 2
+  auto turn = [&](auto buf, int t, f32x16 (&s)[TILE / 32], f32x16 (&next)[TILE / 32]) {   // buf: t % 2
     wait_dma();
     __syncthreads();
     load_k(t + 2, sK[buf]);
     load_v(t + 1, sV[buf ^ 1]);
     if (t >= mine) return;               // wave-uniform
-    const int k0 = (t * KS + set) * GA_TILE;
-    if (k0 + GA_TILE > full_end) {
+    const int k0 = (t * KS + set) * TILE;
+    if (k0 + TILE > full_end) {
       asm volatile("; tile with keys that some query does not see");   // no selects elsewhere
       // register e of a lane: key k0 + 32 kt + 8 (e / 4) + 4 half + e % 4
       const int end = (a.causal ? min(len, q0 + (lane & 31) + 1 + off) : len) - k0 - 4 * half;
 #pragma unroll
-      for (int kt = 0; kt < 2; kt++)
+      for (int kt = 0; kt < TILE / 32; kt++)
 #pragma unroll
         for (int e = 0; e < 16; e++)
           if (32 * kt + 8 * (e >> 2) + (e & 3) >= end) s[kt][e] = -INFINITY;
     }
     float mx = s[0][0];
 #pragma unroll
-    for (int kt = 0; kt < 2; kt++)
+    for (int kt = 0; kt < TILE / 32; kt++)
 #pragma unroll
       for (int e = 0; e < 16; e++) mx = fmaxf(mx, s[kt][e]);
     if (__any(mx > limit)) {
@@ -227,7 +230,7 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_fwd_kernel(GroupedArgs 
     scores(sK[buf ^ 1], next);
     const bf16* tv = sV[buf];
 #pragma unroll
-    for (int kt = 0; kt < 2; kt++) {
+    for (int kt = 0; kt < TILE / 32; kt++) {
 #pragma unroll
       for (int e = 0; e < 16; e++) {
         const float p = __builtin_amdgcn_exp2f(fmaf(s[kt][e], sc, -m));
@@ -239,12 +242,12 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_fwd_kernel(GroupedArgs 
         const bf16x8 pf = att_pack(s[kt], mm);
 #pragma unroll
         for (int d = 0; d < D / 32; d++)
-          o[d] = mfma32(ga_trfrag<GA_TILE>(tv, 32 * kt + 16 * mm, 32 * d, lane), pf, o[d]);
+          o[d] = mfma32(ga_trfrag<TILE>(tv, 32 * kt + 16 * mm, 32 * d, lane), pf, o[d]);
       }
     }
   };
   if (turns) {
-    f32x16 s[2], next[2];
+    f32x16 s[TILE / 32], next[TILE / 32];
     load_k(0, sK[0]);
     load_v(0, sV[0]);
     load_k(1, sK[1]);
@@ -256,33 +259,37 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_fwd_kernel(GroupedArgs 
       if (t + 1 < turns) turn(Const<1>(), t + 1, next, s);
     }
   }
-  if constexpr (KS == 2) {
-    // the second set's sums to the first, through the tiles' place: [wave][register quad][lane]
-    static_assert(sizeof(sKV) >= 4 * (D / 8 + 1) * 64 * sizeof(f32x4), "");
-    f32x4* to = (f32x4*)sKV + wave * (D / 8 + 1) * 64 + lane;
+  if constexpr (KS > 1) {
+    // the other sets' sums to the first, through the tiles' place: [set][wave][register quad][lane]
+    constexpr int QUADS = (D / 8 + 1) * 64;
+    static_assert(sizeof(sKV) >= (KS - 1) * W * QUADS * sizeof(f32x4), "");
+    f32x4* to = (f32x4*)sKV + wave * QUADS + lane;
     __syncthreads();
     if (set) {
+      f32x4* mine = to + (set - 1) * W * QUADS;
 #pragma unroll
       for (int d = 0; d < D / 32; d++)
 #pragma unroll
         for (int g = 0; g < 4; g++)
-          to[(4 * d + g) * 64] = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
-      to[D / 8 * 64] = f32x4{m, l, 0.f, 0.f};
+          mine[(4 * d + g) * 64] = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+      mine[D / 8 * 64] = f32x4{m, l, 0.f, 0.f};
     }
     __syncthreads();
     if (set) return;
-    const f32x4 ml = to[D / 8 * 64];
-    const float mn = fmaxf(m, ml[0]), x = __builtin_amdgcn_exp2f(m - mn), y = __builtin_amdgcn_exp2f(ml[0] - mn);
-    m = mn;
-    l = l * x + ml[1] * y;
+    for (int other = 1; other < KS; other++, to += W * QUADS) {
+      const f32x4 ml = to[D / 8 * 64];
+      const float mn = fmaxf(m, ml[0]), x = __builtin_amdgcn_exp2f(m - mn), y = __builtin_amdgcn_exp2f(ml[0] - mn);
+      m = mn;
+      l = l * x + ml[1] * y;
 #pragma unroll
-    for (int d = 0; d < D / 32; d++)
+      for (int d = 0; d < D / 32; d++)
 #pragma unroll
-      for (int g = 0; g < 4; g++) {
-        const f32x4 v = to[(4 * d + g) * 64];
+        for (int g = 0; g < 4; g++) {
+          const f32x4 v = to[(4 * d + g) * 64];
 #pragma unroll
-        for (int r = 0; r < 4; r++) o[d][4 * g + r] = o[d][4 * g + r] * x + v[r] * y;
-      }
+          for (int r = 0; r < 4; r++) o[d][4 * g + r] = o[d][4 * g + r] * x + v[r] * y;
+        }
+    }
   }
   if (q0 >= a.n_q) return;
   l += __shfl_xor(l, 32);
@@ -323,19 +330,20 @@ __device__ __forceinline__ size_t ga_stats(int bh, int n_q, int row0) {
   return ((size_t)bh * ((n_q + 31) / 32) + row0 / 32) * 64;
 }
 
-template <int D, int KS>
-__global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_q_kernel(GroupedArgs a) {
+template <int D, int W, int KS>
+__global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a) {
+  constexpr int ROWS = 32 * W;
   __shared__ __attribute__((aligned(1024))) bf16 sKV[KS][2][GA_BUFS][GA_STEP * D];   // keys, values
   Item it;
-  if (!ga_item(a.batch, a.q_heads, (a.n_q + GA_ROWS - 1) / GA_ROWS, a.causal, &it)) return;
+  if (!ga_item(a.batch, a.q_heads, (a.n_q + ROWS - 1) / ROWS, a.causal, &it)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = wave_index<GA_THREADS * KS / 64>() & 3, set = wave_index<GA_THREADS * KS / 64>() >> 2;
+  const int wave = wave_index<W * KS>() % W, set = wave_index<W * KS>() / W;
   const int kvh = it.h / a.group, len = ga_length(a, it.b), off = a.n_k - a.n_q;
-  const int blk0 = it.tile * GA_ROWS, q0 = blk0 + 32 * wave;
+  const int blk0 = it.tile * ROWS, q0 = blk0 + 32 * wave;
   const size_t os = (size_t)a.q_heads * D;
   const bf16* kb = a.k + (size_t)it.b * a.n_k * a.k_stride + (size_t)kvh * D;
   const bf16* vb = a.v + (size_t)it.b * a.n_k * a.v_stride + (size_t)kvh * D;
-  const int blk_end = a.causal ? min(len, blk0 + GA_ROWS + off) : len;
+  const int blk_end = a.causal ? min(len, blk0 + ROWS + off) : len;
   const int wave_end = a.causal ? min(len, q0 + 32 + off) : len;
   const int full_end = a.causal ? min(len, q0 + 1 + off) : len;
   // tiles as in the forward
@@ -345,7 +353,7 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_q_kernel(GroupedArg
   const int mine = (wave_tiles - set + KS - 1) / KS;
   bf16(*sK)[GA_STEP * D] = sKV[set][0];
   bf16(*sV)[GA_STEP * D] = sKV[set][1];
-  const TileDma<D, GA_STEP> dk(wave, lane, a.k_stride), dv(wave, lane, a.v_stride);
+  const TileDma<D, GA_STEP, W> dk(wave, lane, a.k_stride), dv(wave, lane, a.v_stride);
   auto load = [&](auto buf, int t) {      // buf: t % GA_BUFS
     if (t >= tiles) return;
     dk.load(kb, a.k_stride, (t * KS + set) * GA_STEP, len, sK[buf]);
@@ -391,13 +399,16 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_q_kernel(GroupedArg
         z += p;
       }
     }
-    if constexpr (KS == 2) {              // the other set's share
-      __shared__ float2 sD[2][4][64];
+    if constexpr (KS > 1) {               // all sets' shares, in one order
+      __shared__ float2 sD[KS][W][64];
       sD[set][wave][lane] = float2{d, z};
       __syncthreads();
-      const float2 other = sD[set ^ 1][wave][lane];
-      d += other.x;
-      z += other.y;
+      d = z = 0.f;
+#pragma unroll
+      for (int i = 0; i < KS; i++) {
+        d += sD[i][wave][lane].x;
+        z += sD[i][wave][lane].y;
+      }
     }
     z += __shfl_xor(z, 32);
   }
@@ -419,7 +430,7 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_q_kernel(GroupedArg
   };
   auto turn = [&](auto buf, int t, f32x16& s, f32x16& dp, f32x16& s_next, f32x16& dp_next) {
     // tile t + 1 has landed when at most t + 2's loads are on their way
-    if (t + 2 < tiles) wait_vmcnt<2 * TileDma<D, GA_STEP>::PER>();
+    if (t + 2 < tiles) wait_vmcnt<2 * TileDma<D, GA_STEP, W>::PER>();
     else wait_vmcnt<0>();
     __syncthreads();
     if (t) load(Const<(buf + 3) % GA_BUFS>(), t + 3);
@@ -452,26 +463,29 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_q_kernel(GroupedArg
       if (t + 3 < turns) turn(Const<3>(), t + 3, s2, dp2, s, dp);
     }
   }
-  if constexpr (KS == 2) {                // as in the forward
-    static_assert(sizeof(sKV) >= 4 * D / 8 * 64 * sizeof(f32x4), "");
-    f32x4* to = (f32x4*)sKV + wave * (D / 8) * 64 + lane;
+  if constexpr (KS > 1) {                 // as in the forward
+    constexpr int QUADS = D / 8 * 64;
+    static_assert(sizeof(sKV) >= (KS - 1) * W * QUADS * sizeof(f32x4), "");
+    f32x4* to = (f32x4*)sKV + wave * QUADS + lane;
     __syncthreads();
     if (set)
 #pragma unroll
       for (int dt = 0; dt < D / 32; dt++)
 #pragma unroll
         for (int g = 0; g < 4; g++)
-          to[(4 * dt + g) * 64] = f32x4{gq[dt][4 * g], gq[dt][4 * g + 1], gq[dt][4 * g + 2], gq[dt][4 * g + 3]};
+          to[(set - 1) * W * QUADS + (4 * dt + g) * 64] =
+              f32x4{gq[dt][4 * g], gq[dt][4 * g + 1], gq[dt][4 * g + 2], gq[dt][4 * g + 3]};
     __syncthreads();
     if (set) return;
+    for (int other = 1; other < KS; other++, to += W * QUADS)
 #pragma unroll
-    for (int dt = 0; dt < D / 32; dt++)
+      for (int dt = 0; dt < D / 32; dt++)
 #pragma unroll
-      for (int g = 0; g < 4; g++) {
-        const f32x4 v = to[(4 * dt + g) * 64];
+        for (int g = 0; g < 4; g++) {
+          const f32x4 v = to[(4 * dt + g) * 64];
 #pragma unroll
-        for (int r = 0; r < 4; r++) gq[dt][4 * g + r] += v[r];
-      }
+          for (int r = 0; r < 4; r++) gq[dt][4 * g + r] += v[r];
+        }
   }
   if (q0 >= a.n_q) return;
   bf16* dqb = a.dq + ((size_t)it.b * a.n_q + q0) * a.dq_stride + (size_t)it.h * D;
@@ -487,8 +501,9 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_q_kernel(GroupedArg
 //
 // A lane's 16 rows have statistics of their own, read from LDS: S and dP start from
 // them instead of 0, which saves the vector unit its subtractions (8 x 4096, 16
-// heads of 64 over 4: 980 us for the whole backward, 1008 without).  KS as in the
-// forward, for head dimension 64 alone: with 128 a SIMD's registers hold one wave.
+// heads of 64 over 4: 980 us for the whole backward, 1008 without).  KS = 2: two
+// sets of four waves where the blocks are few, for head dimension 64 alone: with
+// 128 a SIMD's registers hold one wave.
 template <int D, int KS>
 __global__ __launch_bounds__(GA_THREADS * KS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(GroupedArgs a) {
   __shared__ __attribute__((aligned(1024))) bf16 sQO[KS][2][GA_BUFS][GA_STEP * D];   // queries, dout
@@ -705,10 +720,11 @@ GroupedArgs ga_slice(const GroupedArgs& a, int64_t b0, int64_t nb) {
 }
 
 constexpr int64_t GA_MAX_BLOCKS = 1 << 23;     // of a launch: below 2^32 threads
-// Sets of four waves that share a block's tiles of keys: two where a CU has one
-// block at most.
-int ga_sets(int64_t blocks) { return blocks <= 256 ? 2 : 1; }
+// Whether so few blocks of 128 rows leave a CU with one at most: each is then given
+// more waves.
+bool ga_few(int64_t blocks) { return blocks <= 256; }
 int64_t ga_tiles(int n) { return (n + GA_ROWS - 1) / GA_ROWS; }
+int64_t ga_halves(int n) { return (n + GA_ROWS / 2 - 1) / (GA_ROWS / 2); }
 
 template <int D>
 hipError_t ga_forward(const GroupedArgs& a, hipStream_t st) {
@@ -716,10 +732,10 @@ hipError_t ga_forward(const GroupedArgs& a, hipStream_t st) {
   const int64_t most = GA_MAX_BLOCKS / per > 0 ? GA_MAX_BLOCKS / per : 1;
   for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
     const int64_t nb = a.batch - b0 < most ? a.batch - b0 : most;
-    if (ga_sets(nb * per) == 2)
-      ga_fwd_kernel<D, 2><<<(int)(nb * per), 2 * GA_THREADS, 0, st>>>(ga_slice(a, b0, nb));
+    if (ga_few(nb * per))
+      ga_fwd_kernel<D, 2, 4><<<(int)(nb * ga_halves(a.n_q) * a.q_heads), 512, 0, st>>>(ga_slice(a, b0, nb));
     else
-      ga_fwd_kernel<D, 1><<<(int)(nb * per), GA_THREADS, 0, st>>>(ga_slice(a, b0, nb));
+      ga_fwd_kernel<D, 4, 1><<<(int)(nb * per), 256, 0, st>>>(ga_slice(a, b0, nb));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -751,14 +767,15 @@ hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
   for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
     const int64_t nb = a.batch - b0 < most ? a.batch - b0 : most;
     const GroupedArgs s = ga_slice(a, b0, nb);
-    if (ga_sets(nb * q) == 2)
-      ga_bwd_q_kernel<D, 2><<<(int)(nb * q), 2 * GA_THREADS, 0, st>>>(s);
+    constexpr int QSETS = D == 64 ? 4 : 2;         // as many as the tiles leave LDS for
+    if (ga_few(nb * q))
+      ga_bwd_q_kernel<D, 2, QSETS><<<(int)(nb * ga_halves(a.n_q) * a.q_heads), 128 * QSETS, 0, st>>>(s);
     else
-      ga_bwd_q_kernel<D, 1><<<(int)(nb * q), GA_THREADS, 0, st>>>(s);
+      ga_bwd_q_kernel<D, 4, 1><<<(int)(nb * q), 256, 0, st>>>(s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if constexpr (D == 64) {
-      if (ga_sets(nb * kv) == 2)
+      if (ga_few(nb * kv))
         ga_bwd_kv_kernel<D, 2><<<(int)(nb * kv), 2 * GA_THREADS, 0, st>>>(s);
       else
         ga_bwd_kv_kernel<D, 1><<<(int)(nb * kv), GA_THREADS, 0, st>>>(s);
