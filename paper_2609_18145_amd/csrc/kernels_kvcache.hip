@@ -19,6 +19,8 @@
 // each dimension's row.  So both operands go from memory to registers to the
 // matrix instruction, with no LDS and no transposition, in 16-byte loads of
 // whole lines; the conversion to bf16 multiplies the scale in, exactly.
+#include <algorithm>
+
 #include "hcmix_internal.h"
 #include "device_common.h"
 
@@ -321,18 +323,18 @@ __global__ __launch_bounds__(KV_THREADS) void kv_read_kernel(KvReadArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Attention: a block of four waves takes a range of the sequence's blocks for
-// one key/value head and 16 NQ of its query rows (token, head of the group);
-// its waves take the range's blocks in turn, each with its own running maximum
+// Attention: a block of W waves takes a range of the sequence's blocks for one
+// key/value head and 16 NQ of its query rows (token, head of the group); its
+// waves take the range's blocks in turn, each with its own running maximum
 // and sums, joined at the end.
 // ---------------------------------------------------------------------------
-template <int D, int NQ>
-__global__ __launch_bounds__(KV_THREADS) void kv_attention_kernel(KvAttentionArgs a) {
+template <int D, int NQ, int W>
+__global__ __launch_bounds__(64 * W) void kv_attention_kernel(KvAttentionArgs a) {
   constexpr int KS = D / 32, DT = D / 16;
-  __shared__ float sm[KV_WAVES][16 * NQ], sl[KV_WAVES][16 * NQ];
-  __shared__ __attribute__((aligned(16))) float so[KV_WAVES][16][D + 4];
+  __shared__ float sm[W][16 * NQ], sl[W][16 * NQ];
+  __shared__ __attribute__((aligned(16))) float so[W][16][D + 4];
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int wave = wave_index<KV_WAVES>();
+  const int wave = wave_index<W>();
   const int split = blockIdx.x % a.splits, rt = blockIdx.x / a.splits;
   const int h = blockIdx.y, b = blockIdx.z;
   const int rows = a.tokens * a.group, r0 = rt * 16 * NQ;
@@ -366,7 +368,7 @@ __global__ __launch_bounds__(KV_THREADS) void kv_attention_kernel(KvAttentionArg
     m[j] = -3e38f;
     l[j] = 0.f;
   }
-  for (int blk = lo + wave; blk < hi; blk += KV_WAVES) {
+  for (int blk = lo + wave; blk < hi; blk += W) {
     const size_t at = at0 + blk;
     const unsigned char* ck = a.keys + at * KB * D;
     const unsigned char* cv = a.values + at * KB * D;
@@ -467,15 +469,15 @@ __global__ __launch_bounds__(KV_THREADS) void kv_attention_kernel(KvAttentionArg
 #pragma unroll
     for (int d = 0; d < DT; d++) *(f32x4*)&so[wave][c][16 * d + 4 * g] = o[j][d];
     __syncthreads();
-    for (int i = threadIdx.x; i < 16 * D / 4; i += KV_THREADS) {
+    for (int i = threadIdx.x; i < 16 * D / 4; i += 64 * W) {
       const int row = i / (D / 4), d4 = i % (D / 4), r = r0 + 16 * j + row;
       if (r >= rows) continue;
       float mm = -3e38f, ll = 0.f;
 #pragma unroll
-      for (int w = 0; w < KV_WAVES; w++) mm = fmaxf(mm, sm[w][16 * j + row]);
+      for (int w = 0; w < W; w++) mm = fmaxf(mm, sm[w][16 * j + row]);
       f32x4 acc = {};
 #pragma unroll
-      for (int w = 0; w < KV_WAVES; w++) {
+      for (int w = 0; w < W; w++) {
         const float f = __builtin_amdgcn_exp2f(sm[w][16 * j + row] - mm);
         ll += f * sl[w][16 * j + row];
         acc += f * *(const f32x4*)&so[w][row][4 * d4];
@@ -496,23 +498,41 @@ __global__ __launch_bounds__(KV_THREADS) void kv_attention_kernel(KvAttentionArg
   }
 }
 
-// Joins the ranges of a row: D / 4 threads per row.
-__global__ __launch_bounds__(KV_THREADS) void kv_join_kernel(KvAttentionArgs a, int D, int64_t total) {
-  const int64_t i = (int64_t)blockIdx.x * KV_THREADS + threadIdx.x;
-  const int64_t row = i / (D / 4);
-  const int d4 = (int)(i - row * (D / 4));
-  if (row >= total) return;
+// Joins the ranges of a row, a block to each: D / 4 threads take a range's
+// dimensions, so many such groups the ranges in turn, each with its own maximum.
+template <int D>
+__global__ __launch_bounds__(KV_THREADS) void kv_join_kernel(KvAttentionArgs a) {
+  constexpr int T = D / 4, G = KV_THREADS / T;
+  __shared__ __attribute__((aligned(16))) f32x4 so[G][T];
+  __shared__ float2 sm[G];
+  const int64_t row = blockIdx.x;
+  const int d4 = threadIdx.x % T, g = threadIdx.x / T;
+  const float2* stats = (const float2*)a.stats + row * a.splits;
+  const float* part = a.partial + row * a.splits * D + 4 * d4;
   float mm = -3e38f, ll = 0.f;
-#pragma unroll 8
-  for (int s = 0; s < a.splits; s++) mm = fmaxf(mm, a.stats[2 * (row * a.splits + s)]);
   f32x4 acc = {};
-#pragma unroll 8
-  for (int s = 0; s < a.splits; s++) {
-    const size_t p = row * a.splits + s;
-    const float2 st = *(const float2*)(a.stats + 2 * p);
+  for (int s = g; s < a.splits; s += G) mm = fmaxf(mm, stats[s].x);
+#pragma unroll 4
+  for (int s = g; s < a.splits; s += G) {
+    const float2 st = stats[s];
     const float f = __builtin_amdgcn_exp2f(st.x - mm);
     ll += f * st.y;
-    acc += f * *(const f32x4*)(a.partial + p * D + 4 * d4);
+    acc += f * *(const f32x4*)(part + (size_t)s * D);
+  }
+  so[g][d4] = acc;
+  if (d4 == 0) sm[g] = float2{mm, ll};
+  __syncthreads();
+  if (g) return;
+  mm = sm[0].x;
+#pragma unroll
+  for (int i = 1; i < G; i++) mm = fmaxf(mm, sm[i].x);
+  acc = f32x4{};
+  ll = 0.f;
+#pragma unroll
+  for (int i = 0; i < G; i++) {
+    const float f = __builtin_amdgcn_exp2f(sm[i].x - mm);
+    ll += f * sm[i].y;
+    acc += f * so[i][d4];
   }
   const int rows = a.tokens * a.group;
   const int64_t bh = row / rows, b = bh / a.kv_heads;
@@ -527,31 +547,54 @@ __global__ __launch_bounds__(KV_THREADS) void kv_join_kernel(KvAttentionArgs a, 
 
 int kv_row_tiles(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }     // NQ
 
-// Ranges of a sequence: enough blocks of threads for the chip and, where several
-// fit a CU, twice as many, since the lengths of a batch differ (32 sequences up to
-// 16384 long, 8 heads of 128: 109.9 us with 512 blocks, 105.9 with 1024; 64 query
-// rows of 8 x 8192, which take a CU each: 38.5 with 256, 44.4 with 512); each with
-// at least two of the sequence's blocks for every wave.
-int kv_splits(int64_t batch, int kv_heads, int rows, int max_length) {
-  const int nq = kv_row_tiles(rows);
-  const int64_t blocks = batch * kv_heads * ((rows + 16 * nq - 1) / (16 * nq));
-  const int64_t want = (1024 / nq + blocks - 1) / blocks;
-  const int64_t most = ((max_length + KB - 1) / KB + 2 * KV_WAVES - 1) / (2 * KV_WAVES);
-  const int64_t s = want < most ? want : most;
-  return s < 1 ? 1 : (int)s;
+// How a call is cut: the ranges of a sequence, and the waves of a block.
+//
+// Ranges: enough blocks of threads for the chip and, where several fit a CU, twice
+// as many, since the lengths of a batch differ (32 sequences up to 16384 long, 8
+// heads of 128: 109.9 us with 512 blocks, 105.9 with 1024; 64 query rows of
+// 8 x 8192, which take a CU each: 38.5 with 256, 44.4 with 512).  A range has one
+// of the sequence's blocks for every wave up to 16 ranges (a wave's second block
+// is loaded after the first: 1 x 4000, 32 heads of 128 over 8: 10.2 us with two,
+// 8.7), two where that makes more (4 x 8000: 13.6, one: 14.9).
+//
+// Waves: a block of 16, or of 8 where head dimension or rows leave 16 too few
+// registers, takes a sequence by itself where none of its waves gets more than one
+// and a half blocks, or four where such blocks fill the chip: no partial sums, no
+// second kernel.  us with four waves and ranges, and so: 1 x 700, 8 heads of 64
+// over 2 7.0, 5.5; 16 x 1000, 8 of 64 over 8 8.4, 7.0; 32 x 2000, 32 of 128 over 8,
+// 6 tokens 31.3, 25.1 (but 1 x 1500, 32 of 128 over 8 8.6, 14.4).
+struct KvPlan {
+  int splits, waves;
+};
+KvPlan kv_plan(int64_t batch, int kv_heads, int rows, int max_length, int D) {
+  const int nq = kv_row_tiles(rows), blocks = (max_length + KB - 1) / KB;
+  const int64_t sequences = batch * kv_heads, tiles = sequences * ((rows + 16 * nq - 1) / (16 * nq));
+  const int64_t want = (1024 / nq + tiles - 1) / tiles;
+  const int64_t per = (blocks + KV_WAVES - 1) / KV_WAVES;
+  const int64_t s = std::min(want, std::max(std::min<int64_t>(per, 16), (per + 1) / 2));
+  const int w = D == 64 && nq == 1 ? 16 : 8;
+  if (s > 1 && nq <= 2 && blocks <= w * (sequences < 256 ? 3 : 8) / 2) return {1, w};
+  return {s < 1 ? 1 : (int)s, KV_WAVES};
 }
 
 template <int D>
-hipError_t kv_attention_launch(const KvAttentionArgs& a, hipStream_t st) {
+hipError_t kv_attention_launch(const KvAttentionArgs& a, int waves, hipStream_t st) {
   const int rows = a.tokens * a.group, nq = kv_row_tiles(rows);
   const dim3 grid(a.splits * ((rows + 16 * nq - 1) / (16 * nq)), a.kv_heads, a.batch);
-  if (nq == 1) kv_attention_kernel<D, 1><<<grid, KV_THREADS, 0, st>>>(a);
-  else if (nq == 2) kv_attention_kernel<D, 2><<<grid, KV_THREADS, 0, st>>>(a);
-  else kv_attention_kernel<D, 4><<<grid, KV_THREADS, 0, st>>>(a);
+  if (waves > KV_WAVES) {
+    constexpr int W1 = D == 64 ? 16 : 8;
+    if (nq == 1) kv_attention_kernel<D, 1, W1><<<grid, 64 * W1, 0, st>>>(a);
+    else kv_attention_kernel<D, 2, 8><<<grid, 512, 0, st>>>(a);
+  } else if (nq == 1) {
+    kv_attention_kernel<D, 1, KV_WAVES><<<grid, KV_THREADS, 0, st>>>(a);
+  } else if (nq == 2) {
+    kv_attention_kernel<D, 2, KV_WAVES><<<grid, KV_THREADS, 0, st>>>(a);
+  } else {
+    kv_attention_kernel<D, 4, KV_WAVES><<<grid, KV_THREADS, 0, st>>>(a);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t total = (int64_t)a.batch * a.kv_heads * rows;
-  kv_join_kernel<<<(int)((total * (D / 4) + KV_THREADS - 1) / KV_THREADS), KV_THREADS, 0, st>>>(a, D, total);
+  kv_join_kernel<D><<<(int)(a.batch * a.kv_heads * rows), KV_THREADS, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -579,7 +622,7 @@ hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t st) {
 
 size_t kv_attention_workspace_bytes(int64_t batch, int32_t kv_heads, int32_t group,
                                     int32_t head_dim, int32_t tokens, int32_t max_length) {
-  const int splits = kv_splits(batch, kv_heads, tokens * group, max_length);
+  const int splits = kv_plan(batch, kv_heads, tokens * group, max_length, head_dim).splits;
   if (splits == 1) return 0;
   const size_t parts = (size_t)batch * kv_heads * tokens * group * splits;
   return parts * (head_dim + 2) * sizeof(float) / 256 * 256 + 256;
@@ -587,10 +630,12 @@ size_t kv_attention_workspace_bytes(int64_t batch, int32_t kv_heads, int32_t gro
 
 hipError_t launch_kv_attention(KvAttentionArgs a, void* workspace, int32_t max_length,
                                hipStream_t st) {
-  a.splits = kv_splits(a.batch, a.kv_heads, a.tokens * a.group, max_length);
+  const KvPlan plan = kv_plan(a.batch, a.kv_heads, a.tokens * a.group, max_length, a.head_dim);
+  a.splits = plan.splits;
   a.partial = (float*)workspace;
   a.stats = a.partial + (size_t)a.batch * a.kv_heads * a.tokens * a.group * a.splits * a.head_dim;
-  return a.head_dim == 64 ? kv_attention_launch<64>(a, st) : kv_attention_launch<128>(a, st);
+  return a.head_dim == 64 ? kv_attention_launch<64>(a, plan.waves, st)
+                          : kv_attention_launch<128>(a, plan.waves, st);
 }
 
 }  // namespace hcmix

@@ -139,6 +139,10 @@ ATTENTION = [
     (1, 700, 12, 4, 128, 30, [650], None), (2, 200, 3, 3, 64, 130, [200, 131], None),
     (2, 90, 4, 2, 64, 2, [-7, 1000], None), (1, 2100, 32, 1, 128, 1, [2050], 2100),
     (1, 2100, 64, 1, 128, 2, [2050], 2100),
+    # blocks of 16 and of 8 waves that have a sequence each; 18 ranges
+    (5, 777, 4, 2, 64, 1, [777, 0, 300, 1, 700], None), (2, 700, 20, 1, 128, 1, [700, 10], None),
+    (64, 1000, 8, 4, 64, 2, [1000 - 9 * i for i in range(64)], None), (1, 9000, 4, 1, 64, 1, [8800], None),
+    (3, 700, 20, 1, 64, 1, [64, 700, 449], 700),
 ]
 
 
