@@ -501,11 +501,13 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
 //
 // A lane's 16 rows have statistics of their own, read from LDS: S and dP start from
 // them instead of 0, which saves the vector unit its subtractions (8 x 4096, 16
-// heads of 64 over 4: 980 us for the whole backward, 1008 without).  KS = 2: two
-// sets of four waves where the blocks are few, for head dimension 64 alone: with
-// 128 a SIMD's registers hold one wave.
-template <int D, int KS>
-__global__ __launch_bounds__(GA_THREADS * KS, D == 64 ? 2 : 1) void ga_bwd_kv_kernel(GroupedArgs a) {
+// heads of 64 over 4: 980 us for the whole backward, 1008 without).
+//
+// Head dimension 64: a wave makes all four products of its 32 keys.  KS = 2: two
+// sets of four waves share the query tiles where the blocks are few.
+template <int KS>
+__global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_kv_kernel(GroupedArgs a) {
+  constexpr int D = 64;
   __shared__ __attribute__((aligned(1024))) bf16 sQO[KS][2][GA_BUFS][GA_STEP * D];   // queries, dout
   // a tile's statistics, four times over: every wave copies them, to keep one
   // count of loads on their way, and 64 lanes copy 1 KB
@@ -605,10 +607,6 @@ __global__ __launch_bounds__(GA_THREADS * KS, D == 64 ? 2 : 1) void ga_bwd_kv_ke
         dk[d] = mfma32(ga_trfrag<GA_STEP>(tq, 16 * mm, 32 * d, lane), sf, dk[d]);
       }
     }
-    // the compiler's order for matrix products fed from LDS: with head dimension
-    // 128 a wave is alone on its SIMD (8 x 4096, 8 heads over 2: 1030 us for the
-    // backward, 977 so; 64: the same either way)
-    __builtin_amdgcn_iglp_opt(0);
   };
   if (turns > 0) {
     f32x16 s, dp, s2, dp2;
@@ -673,6 +671,156 @@ __global__ __launch_bounds__(GA_THREADS * KS, D == 64 ? 2 : 1) void ga_bwd_kv_ke
     att_store(dkb + 32 * d, a.dk_stride, dk[d], a.scale, lane, a.n_k - j0);
     att_store(dvb + 32 * d, a.dv_stride, dv[d], 1.f, lane, a.n_k - j0);
   }
+}
+
+// Head dimension 128: all four products of 32 keys take more than half of a SIMD's
+// registers, and a wave that is alone there waits for itself.  So two waves of one
+// SIMD share them: the first makes S, P and dV, the second dP, dS and dK a turn
+// later, from the P in fp32 that the first leaves in LDS.  The tiles of two turns
+// back, now and the next are in use, the fourth buffer's is on its way.  (8 x 4096,
+// 8 heads over 2: the backward 970 us with a wave for all four, 909 so, 925 without
+// the hint on order; 32 x 512: 122, 113; by head dimension 64 952 and 1064: there
+// the exchange costs more LDS than it hides.)
+__global__ __launch_bounds__(512, 2) void ga_bwd_pair_kernel(GroupedArgs a) {
+  constexpr int D = 128;
+  __shared__ __attribute__((aligned(1024))) bf16 sT[GA_BUFS][2][GA_STEP * D];   // queries, dout
+  __shared__ __attribute__((aligned(1024))) float sS[GA_BUFS][256];
+  __shared__ __attribute__((aligned(1024))) f32x4 sP[2][4][4][64];              // [turn % 2][wave][quad][lane]
+  Item it;
+  const int key_tiles = (a.n_k + GA_ROWS - 1) / GA_ROWS;
+  if (!ga_item(a.batch, a.kv_heads, key_tiles * a.parts, false, &it)) return;
+  const int part = it.tile % a.parts;
+  it.tile /= a.parts;
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = wave_index<8>() & 3, role = wave_index<8>() >> 2;
+  const int len = ga_length(a, it.b), off = a.n_k - a.n_q;
+  const int blk0 = it.tile * GA_ROWS, j0 = blk0 + 32 * wave, j = j0 + (lane & 31);
+  const size_t os = (size_t)a.q_heads * D;
+  bf16x8 xf[D / 16];
+  if (role == 0)
+    ga_rows<D>(xf, a.k + (size_t)it.b * a.n_k * a.k_stride + (size_t)it.h * D, a.k_stride, j0, len, lane);
+  else
+    ga_rows<D>(xf, a.v + (size_t)it.b * a.n_k * a.v_stride + (size_t)it.h * D, a.v_stride, j0, len, lane);
+  f32x16 acc[D / 32] = {};
+  const float sc = a.scale * GA_LOG2E;
+  const int first = a.causal && blk0 - off > 0 ? (blk0 - off) / GA_STEP : 0;
+  const int per = blk0 < len ? max(0, (a.n_q + GA_STEP - 1) / GA_STEP - first) : 0;
+  const int lo = (int)((int64_t)per * a.group * part / a.parts);
+  const int hi = (int)((int64_t)per * a.group * (part + 1) / a.parts);
+  const int steps = hi - lo;
+  const int64_t stride = role ? (int64_t)os : a.q_stride;
+  const bf16* src = role ? a.dout + (size_t)it.b * a.n_q * os : a.q + (size_t)it.b * a.n_q * a.q_stride;
+  const TileDma<D, GA_STEP> dma(wave, lane, stride);
+  int lg = per ? lo / per : 0, lt = lo - lg * per;       // head and tile to be loaded next
+  int ct = lt;                                           // tile to be computed next
+  auto load = [&](auto buf, int step) {                  // buf: step % GA_BUFS
+    if (step >= steps) return;
+    const int h = it.h * a.group + lg, i0 = (first + lt) * GA_STEP;
+    dma.load(src + (size_t)h * D, stride, i0, a.n_q, sT[buf][role]);
+    if (wave == 0 && role == 0)
+      dma16_at((const bf16*)(a.stats + ga_stats(it.b * a.q_heads + h, a.n_q, i0)), 16 * (lane & 15),
+               (bf16*)sS[buf]);
+    if (++lt == per) {
+      lt = 0;
+      lg++;
+    }
+  };
+  auto product = [&](auto buf, f32x16& x) {              // S or dP
+#pragma unroll
+    for (int g = 0; g < 4; g++) {
+      const f32x4 y = *(const f32x4*)(sS[buf] + 32 * role + 8 * g + 4 * half);
+#pragma unroll
+      for (int r = 0; r < 4; r++) x[4 * g + r] = y[r];
+    }
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ks++) x = mfma32(ga_frag<GA_STEP>(sT[buf][role], 0, 16 * ks, lane), xf[ks], x);
+  };
+  auto gather = [&](auto buf, const f32x16& x) {         // dV or dK
+#pragma unroll
+    for (int mm = 0; mm < 2; mm++) {
+      const bf16x8 f = att_pack(x, mm);
+#pragma unroll
+      for (int d = 0; d < D / 32; d++)
+        acc[d] = mfma32(ga_trfrag<GA_STEP>(sT[buf][role ^ 1], 16 * mm, 32 * d, lane), f, acc[d]);
+    }
+  };
+  auto meet = [&](auto buf, int t) {
+    wait_dma();
+    __syncthreads();
+    load(Const<(buf + 2) % GA_BUFS>(), t + 2);
+  };
+  auto turn_s = [&](auto buf, int t, f32x16& s, f32x16& next) {
+    meet(buf, t);
+    if (t >= steps) return;
+    const int r0 = (first + ct) * GA_STEP;
+    if (++ct == per) ct = 0;
+    if (j0 + 32 > len || (a.causal && r0 + off < j0 + 31)) {
+      asm volatile("; tile with keys that some query does not see");
+      const int from = j >= len ? 1 << 30 : a.causal ? j - off - r0 : -1;
+#pragma unroll
+      for (int e = 0; e < 16; e++)
+        if (8 * (e >> 2) + 4 * half + (e & 3) < from) s[e] = -INFINITY;
+    }
+    product(Const<(buf + 1) % GA_BUFS>(), next);
+#pragma unroll
+    for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(s[e] * sc);
+#pragma unroll
+    for (int g = 0; g < 4; g++) sP[buf & 1][wave][g][lane] = f32x4{s[4 * g], s[4 * g + 1], s[4 * g + 2], s[4 * g + 3]};
+    gather(buf, s);
+    __builtin_amdgcn_iglp_opt(0);          // the compiler's order for matrix products fed from LDS
+  };
+  auto turn_d = [&](auto buf, int t, f32x16& dp, f32x16& last) {
+    meet(buf, t);
+    product(buf, dp);
+    if (t == 0) return;
+#pragma unroll
+    for (int g = 0; g < 4; g++) {
+      const f32x4 p = sP[(buf + 1) & 1][wave][g][lane];
+#pragma unroll
+      for (int r = 0; r < 4; r++) last[4 * g + r] *= p[r];
+    }
+    gather(Const<(buf + 3) % GA_BUFS>(), last);
+    __builtin_amdgcn_iglp_opt(0);
+  };
+  if (steps > 0) {
+    load(Const<0>(), 0);
+    load(Const<1>(), 1);
+    wait_dma();
+    __syncthreads();
+    f32x16 x, y;
+    if (role == 0) {
+      product(Const<0>(), x);
+      for (int t = 0; t <= steps; t += 4) {
+        turn_s(Const<0>(), t, x, y);
+        if (t + 1 <= steps) turn_s(Const<1>(), t + 1, y, x);
+        if (t + 2 <= steps) turn_s(Const<2>(), t + 2, x, y);
+        if (t + 3 <= steps) turn_s(Const<3>(), t + 3, y, x);
+      }
+    } else {
+      for (int t = 0; t <= steps; t += 4) {
+        turn_d(Const<0>(), t, x, y);
+        if (t + 1 <= steps) turn_d(Const<1>(), t + 1, y, x);
+        if (t + 2 <= steps) turn_d(Const<2>(), t + 2, x, y);
+        if (t + 3 <= steps) turn_d(Const<3>(), t + 3, y, x);
+      }
+    }
+  }
+  if (j0 >= a.n_k) return;
+  if (a.parts > 1) {
+    const size_t rows = (size_t)a.batch * a.n_k * a.kv_heads * D;
+    float* p = a.partial + (2 * part + (role == 0)) * rows + (((size_t)it.b * a.n_k + j) * a.kv_heads + it.h) * D + 4 * half;
+    if (j < a.n_k)
+#pragma unroll
+      for (int d = 0; d < D / 32; d++)
+#pragma unroll
+        for (int g = 0; g < 4; g++)
+          *(f32x4*)(p + 32 * d + 8 * g) = f32x4{acc[d][4 * g], acc[d][4 * g + 1], acc[d][4 * g + 2], acc[d][4 * g + 3]};
+    return;
+  }
+  const int64_t ostride = role ? a.dk_stride : a.dv_stride;
+  bf16* ob = (role ? a.dk : a.dv) + ((size_t)it.b * a.n_k + j0) * ostride + (size_t)it.h * D;
+#pragma unroll
+  for (int d = 0; d < D / 32; d++) att_store(ob + 32 * d, ostride, acc[d], role ? a.scale : 1.f, lane, a.n_k - j0);
 }
 
 // Adds the parts of dK (blockIdx.y 0) or dV, eight columns to a thread.
@@ -776,11 +924,11 @@ hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
     if (e != hipSuccess) return e;
     if constexpr (D == 64) {
       if (ga_few(nb * kv))
-        ga_bwd_kv_kernel<D, 2><<<(int)(nb * kv), 2 * GA_THREADS, 0, st>>>(s);
+        ga_bwd_kv_kernel<2><<<(int)(nb * kv), 2 * GA_THREADS, 0, st>>>(s);
       else
-        ga_bwd_kv_kernel<D, 1><<<(int)(nb * kv), GA_THREADS, 0, st>>>(s);
+        ga_bwd_kv_kernel<1><<<(int)(nb * kv), GA_THREADS, 0, st>>>(s);
     } else {
-      ga_bwd_kv_kernel<D, 1><<<(int)(nb * kv), GA_THREADS, 0, st>>>(s);
+      ga_bwd_pair_kernel<<<(int)(nb * kv), 512, 0, st>>>(s);
     }
     e = hipGetLastError();
     if (e != hipSuccess) return e;
