@@ -503,27 +503,29 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
 // them instead of 0, which saves the vector unit its subtractions (8 x 4096, 16
 // heads of 64 over 4: 980 us for the whole backward, 1008 without).
 //
-// Head dimension 64: a wave makes all four products of its 32 keys.  KS = 2: two
-// sets of four waves share the query tiles where the blocks are few.
-template <int KS>
-__global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_kv_kernel(GroupedArgs a) {
-  constexpr int D = 64;
+// Head dimension 64: a wave makes all four products of its 32 keys.  W and KS as in
+// the forward: where the blocks are few, two waves of keys by four sets that share
+// the query tiles (8 x 1024, 16 heads over 4: 108 us for the whole backward with
+// four by two, 94 so; 1 x 256, 8 heads 20.4, 19.3).
+template <int W, int KS>
+__global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_kv_kernel(GroupedArgs a) {
+  constexpr int D = 64, ROWS = 32 * W;
   __shared__ __attribute__((aligned(1024))) bf16 sQO[KS][2][GA_BUFS][GA_STEP * D];   // queries, dout
   // a tile's statistics, four times over: every wave copies them, to keep one
   // count of loads on their way, and 64 lanes copy 1 KB
   __shared__ __attribute__((aligned(1024))) float sST[KS][GA_BUFS][256];
   Item it;
-  const int key_tiles = (a.n_k + GA_ROWS - 1) / GA_ROWS;
+  const int key_tiles = (a.n_k + ROWS - 1) / ROWS;
   if (!ga_item(a.batch, a.kv_heads, key_tiles * a.parts, false, &it)) return;
   const int part = it.tile % a.parts;
   it.tile /= a.parts;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = wave_index<GA_THREADS * KS / 64>() & 3, set = wave_index<GA_THREADS * KS / 64>() >> 2;
+  const int wave = wave_index<W * KS>() % W, set = wave_index<W * KS>() / W;
   bf16(*sQ)[GA_STEP * D] = sQO[set][0];
   bf16(*sO)[GA_STEP * D] = sQO[set][1];
   float(*sS)[256] = sST[set];
   const int len = ga_length(a, it.b), off = a.n_k - a.n_q;
-  const int blk0 = it.tile * GA_ROWS, j0 = blk0 + 32 * wave, j = j0 + (lane & 31);
+  const int blk0 = it.tile * ROWS, j0 = blk0 + 32 * wave, j = j0 + (lane & 31);
   const size_t os = (size_t)a.q_heads * D;
   bf16x8 kf[D / 16], vf[D / 16];
   ga_rows<D>(kf, a.k + (size_t)it.b * a.n_k * a.k_stride + (size_t)it.h * D, a.k_stride, j0, len, lane);
@@ -538,7 +540,7 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_kv_kernel(GroupedAr
   const int lo = (int)((int64_t)per * a.group * part / a.parts);
   const int hi = (int)((int64_t)per * a.group * (part + 1) / a.parts);
   const int turns = (hi - lo + KS - 1) / KS, steps = (hi - lo - set + KS - 1) / KS;
-  const TileDma<D, GA_STEP> dq(wave, lane, a.q_stride), dout(wave, lane, os);
+  const TileDma<D, GA_STEP, W> dq(wave, lane, a.q_stride), dout(wave, lane, os);
   int lg = per ? (lo + set) / per : 0, lt = lo + set - lg * per;   // head and tile to be loaded next
   int ct = lt;                                                     // tile to be computed next
   auto load = [&](auto buf, int step) {                   // buf: step % GA_BUFS
@@ -575,7 +577,7 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_kv_kernel(GroupedAr
     }
   };
   auto turn = [&](auto buf, int step, f32x16& s, f32x16& dp, f32x16& s_next, f32x16& dp_next) {
-    if (step + 2 < steps) wait_vmcnt<2 * TileDma<D, GA_STEP>::PER + 1>();
+    if (step + 2 < steps) wait_vmcnt<2 * TileDma<D, GA_STEP, W>::PER + 1>();
     else wait_vmcnt<0>();
     __syncthreads();
     load(Const<(buf + 3) % GA_BUFS>(), step + 3);
@@ -623,31 +625,35 @@ __global__ __launch_bounds__(GA_THREADS * KS, 2) void ga_bwd_kv_kernel(GroupedAr
       if (t + 3 < turns) turn(Const<3>(), t + 3, s2, dp2, s, dp);
     }
   }
-  if constexpr (KS == 2) {               // as in the forward
-    static_assert(sizeof(sQO) >= 4 * 2 * D / 8 * 64 * sizeof(f32x4), "");
-    f32x4* to = (f32x4*)sQO + wave * (D / 4) * 64 + lane;
+  if constexpr (KS > 1) {                // as in the forward
+    constexpr int QUADS = D / 4 * 64;
+    static_assert(sizeof(sQO) >= (KS - 1) * W * QUADS * sizeof(f32x4), "");
+    f32x4* to = (f32x4*)sQO + wave * QUADS + lane;
     __syncthreads();
-    if (set)
+    if (set) {
+      f32x4* mine = to + (set - 1) * W * QUADS;
 #pragma unroll
       for (int d = 0; d < D / 32; d++)
 #pragma unroll
         for (int g = 0; g < 4; g++) {
-          to[(8 * d + g) * 64] = f32x4{dk[d][4 * g], dk[d][4 * g + 1], dk[d][4 * g + 2], dk[d][4 * g + 3]};
-          to[(8 * d + 4 + g) * 64] = f32x4{dv[d][4 * g], dv[d][4 * g + 1], dv[d][4 * g + 2], dv[d][4 * g + 3]};
+          mine[(8 * d + g) * 64] = f32x4{dk[d][4 * g], dk[d][4 * g + 1], dk[d][4 * g + 2], dk[d][4 * g + 3]};
+          mine[(8 * d + 4 + g) * 64] = f32x4{dv[d][4 * g], dv[d][4 * g + 1], dv[d][4 * g + 2], dv[d][4 * g + 3]};
         }
+    }
     __syncthreads();
     if (set) return;
+    for (int other = 1; other < KS; other++, to += W * QUADS)
 #pragma unroll
-    for (int d = 0; d < D / 32; d++)
+      for (int d = 0; d < D / 32; d++)
 #pragma unroll
-      for (int g = 0; g < 4; g++) {
-        const f32x4 x = to[(8 * d + g) * 64], y = to[(8 * d + 4 + g) * 64];
+        for (int g = 0; g < 4; g++) {
+          const f32x4 x = to[(8 * d + g) * 64], y = to[(8 * d + 4 + g) * 64];
 #pragma unroll
-        for (int r = 0; r < 4; r++) {
-          dk[d][4 * g + r] += x[r];
-          dv[d][4 * g + r] += y[r];
+          for (int r = 0; r < 4; r++) {
+            dk[d][4 * g + r] += x[r];
+            dv[d][4 * g + r] += y[r];
+          }
         }
-      }
   }
   if (j0 >= a.n_k) return;
   if (a.parts > 1) {
@@ -890,15 +896,22 @@ hipError_t ga_forward(const GroupedArgs& a, hipStream_t st) {
   return hipSuccess;
 }
 
-// Blocks that share a key tile where the tiles are fewer than the CUs: as many as
-// the chip holds at once (two to a CU, one for head dimension 128), each with four
-// query tiles at least.  (5 x 333 x 777, 8 heads of 128 over 2: the backward took
-// 60 us with 256 blocks, 72 with 512; 4 x 1024, 16 heads of 64 over 4: 70 and 66.)
+// Blocks that share a key tile where the tiles are fewer than the CUs.  Every part
+// adds fp32 sums to write and to join, so it has to be worth its steps (query tiles
+// of 32, of all the group's heads).
+//
+// Head dimension 64: a block of eight waves to each CU if a part keeps 16 steps,
+// two to each, which evens out what a causal mask makes uneven, if it keeps 64.  us
+// of the backward with 512 blocks of four waves, and so, 8 heads over 2: 4 x 500
+// 36.5, 28.8; 1 x 1000 42.4, 32.6; 16 x 512 46.4, 40.0; 16 over 4: 4 x 1024 65.4,
+// 63.0; 1 x 4096 186, 171 (one block to each CU 214).
+// Head dimension 128: one block to each CU, 8 steps (5 x 333 x 777, 8 over 2: 51.9,
+// with 16 56.6; 1 x 1000 47.8, 53.0).
 int ga_parts(int64_t batch, int64_t n_q, int64_t n_k, int q_heads, int kv_heads, int head_dim) {
   const int64_t blocks = batch * kv_heads * ga_tiles((int)n_k);
   const int64_t steps = (n_q + GA_STEP - 1) / GA_STEP * (q_heads / kv_heads);
-  const int64_t want = blocks < 256 ? (head_dim == 64 ? 512 : 256) / blocks : 1, most = steps / 4;
-  const int64_t p = want < most ? want : most;
+  const int64_t p = head_dim == 64 ? std::max(std::min(128 / blocks, steps / 16), std::min(256 / blocks, steps / 64))
+                                   : std::min(256 / blocks, steps / 8);
   return p < 1 ? 1 : p > 32 ? 32 : (int)p;
 }
 
@@ -924,9 +937,9 @@ hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
     if (e != hipSuccess) return e;
     if constexpr (D == 64) {
       if (ga_few(nb * kv))
-        ga_bwd_kv_kernel<2><<<(int)(nb * kv), 2 * GA_THREADS, 0, st>>>(s);
+        ga_bwd_kv_kernel<2, 4><<<(int)(nb * ga_halves(a.n_k) * a.kv_heads * a.parts), 512, 0, st>>>(s);
       else
-        ga_bwd_kv_kernel<1><<<(int)(nb * kv), GA_THREADS, 0, st>>>(s);
+        ga_bwd_kv_kernel<4, 1><<<(int)(nb * kv), 256, 0, st>>>(s);
     } else {
       ga_bwd_pair_kernel<<<(int)(nb * kv), 512, 0, st>>>(s);
     }

@@ -41,12 +41,12 @@ def test_grouped_backward(launches, batch, n, heads, kv, hd):  # noqa: F811
 
 
 def test_key_tiles_that_are_shared(launches):  # noqa: F811
-    """Query blocks of 64 rows; 16 key tiles and 512 turns over the queries: 32 blocks to
+    """Blocks of 64 rows; 32 tiles of keys and 512 steps over the queries: 8 blocks to
     each, and their join."""
     ls = launches("hcmix_grouped_attention_backward",
                   forward(1, 4096, 1024, 8, 2, 64, 512) + [mem(5), mem(6)] + i64(512) + [mem(7)]
                   + i64(128) + [mem(8)] + i64(128) + [mem(9), ["size_t", 1 << 39], NONE])
-    assert [x for (x, _, _), _, _ in ls] == [64 * 8, 16 * 32, 1024 * 128 // 8 // 256]
+    assert [x for (x, _, _), _, _ in ls] == [64 * 8, 32 * 8, 1024 * 128 // 8 // 256]
     assert ls[2][0][1] == 2
 
 
