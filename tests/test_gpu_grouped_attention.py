@@ -82,6 +82,25 @@ def test_matches_the_oracle(case):
     check(*draw(batch, n_q, n_k, heads, kv, hd, seed=n_q + n_k, size=size), causal, lengths)
 
 
+def spread(batch, n):
+    """Lengths from 0 past n, none of them round."""
+    return [0, n, n + 5] + [1 + (37 * i) % n for i in range(3, batch)]
+
+
+# more blocks of 128 rows and of 128 keys than the GPU has CUs: blocks of four waves
+MANY = [
+    (70, 130, 260, 4, 2, 64, True, spread(70, 260), 1.0), (70, 260, 130, 4, 2, 128, False, spread(70, 130), 1.0),
+    (66, 290, 300, 4, 2, 64, True, spread(66, 300), 2.0), (66, 300, 300, 4, 2, 128, True, None, 1.0),
+]
+
+
+@pytest.mark.parametrize("case", MANY, ids=lambda c: "x".join(map(str, c[:6])))
+def test_many_blocks_match_the_oracle(case):
+    print(f"case: grouped attention {case[:7]}", flush=True)
+    batch, n_q, n_k, heads, kv, hd, causal, lengths, size = case
+    check(*draw(batch, n_q, n_k, heads, kv, hd, seed=n_q + n_k, size=size), causal, lengths)
+
+
 def test_long_window_sampled():
     """A sequence of 4096; the last head of the last group checked whole."""
     q, k, v, do = draw(1, 4096, 4096, 4, 2, 64, seed=9)
