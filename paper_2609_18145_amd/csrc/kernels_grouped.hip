@@ -217,7 +217,8 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; e++) mx = fmaxf(mx, s[kt][e]);
     if (__any(mx > limit)) {
-      const float mn = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32)) * sc);
+      // of the rows whose own scores ask for it: a row's result does not depend on others
+      const float top = fmaxf(mx, __shfl_xor(mx, 32)), mn = top > limit ? fmaxf(m, top * sc) : m;
       const float alpha = __builtin_amdgcn_exp2f(m - mn);
       m = mn;
       limit = (mn + GA_SLACK) / sc;

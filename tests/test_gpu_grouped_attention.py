@@ -176,10 +176,12 @@ def test_what_lies_behind_the_lengths_is_not_taken(fill):
     assert (res[1][3][0, 37:] == 0).all() and (res[1][4][1, 64:] == 0).all()
 
 
-def test_rows_do_not_see_ahead():
-    q, k, v, _ = draw(1, 300, 300, 2, 1, 128, seed=4)
+@pytest.mark.parametrize("batch,hd,size", [(1, 128, 1.0), (1, 64, 1.0), (1, 64, 6.0), (50, 64, 6.0), (50, 128, 6.0)])
+def test_rows_do_not_see_ahead(batch, hd, size):
+    """Bit for bit, also where later rows of a wave rescale their sums (large scores)."""
+    q, k, v, _ = draw(batch, 300, 300, 2, 1, hd, seed=4, size=size)
     a, la = hcmix.grouped_attention_forward(q, k, v)
-    for i in (0, 63, 64, 200):
+    for i in (0, 1, 17, 63, 64, 200, 280):
         k2, v2 = k.clone(), v.clone()
         k2[:, i + 1:], v2[:, i + 1:] = 5.0, -3.0
         b, lb = hcmix.grouped_attention_forward(q, k2, v2)
