@@ -141,12 +141,11 @@ __device__ __forceinline__ void ga_rows(bf16x8 (&f)[D / 16], const bf16* base, s
 // lanes of a query, is a rare branch.
 //
 // A block is W waves of queries by KS sets that share its key tiles in turn and
-// join at the end: 4 by 1, and 2 by 4 where the blocks of 128 queries are no more
-// than the CUs.  Then a wave alone on its SIMD waits for itself, and a block's
-// whole length is the call's time.  us with 4 by 1, 4 by 2 and 2 by 4, causal, 8
-// heads over 2: 3 x 1000 of 128 23.7, 21.0, 22.0; 1 x 1000 of 64 (4 by 2:) 13.3,
-// 10.4; 2 x 2048 of 64 23.8, 20.8; 1 x 4000 of 128 58.1, 52.3; 4 x 64 queries of
-// 2000 keys of 128 30.5, 22.8.
+// join at the end: 4 by 1, and where the blocks are few, so that a wave alone on
+// its SIMD waits for itself and the longest block is the call's time, 2 by 4 (head
+// dimension 64) or 2 by 2.  us, causal, 8 heads over 2, with 4 by 2, 2 by 4, 2 by
+// 2: 1 x 1000 of 64 13.3, 10.8, 11.9; 2 x 2048 of 64 23.8, 21.0, 22.1; 3 x 1000 of
+// 128 21.0, 21.4, 17.5; 2 x 2048 of 128 34.8, 32.0, 29.8.
 constexpr float GA_SLACK = 8.f;
 
 template <int D, int W, int KS>
@@ -875,9 +874,17 @@ GroupedArgs ga_slice(const GroupedArgs& a, int64_t b0, int64_t nb) {
 }
 
 constexpr int64_t GA_MAX_BLOCKS = 1 << 23;     // of a launch: below 2^32 threads
-// Whether so few blocks of 128 rows leave a CU with one at most: each is then given
-// more waves.
-bool ga_few(int64_t blocks) { return blocks <= 256; }
+// Whether blocks of 128 queries are so few that a CU is better given blocks of 64
+// by several sets: where they fill half of the chip, and up to all of it where a
+// causal mask leaves the longest rows to a few.  us of forward and backward with
+// blocks of 128, and so, 8 heads over 2: 1 x 2048 of 64 27.7 + 68.6, 17.2 + 52.5;
+// 2 x 2048 of 128 40.0 + 127, 30.4 + 121; but 16 x 256 of 64 7.8 + 28.5,
+// 9.3 + 34.0 and 4 x 1000 of 128 without mask 23.3 + 85.7, 24.0 + 96.3.
+bool ga_few(const GroupedArgs& a, int64_t blocks) {
+  return blocks <= (a.causal && a.n_q >= 768 ? 256 : 128);
+}
+// As many sets as the tiles leave LDS for, two blocks to a CU with head dimension 128.
+constexpr int ga_sets(int D) { return D == 64 ? 4 : 2; }
 int64_t ga_tiles(int n) { return (n + GA_ROWS - 1) / GA_ROWS; }
 int64_t ga_halves(int n) { return (n + GA_ROWS / 2 - 1) / (GA_ROWS / 2); }
 
@@ -887,8 +894,8 @@ hipError_t ga_forward(const GroupedArgs& a, hipStream_t st) {
   const int64_t most = GA_MAX_BLOCKS / per > 0 ? GA_MAX_BLOCKS / per : 1;
   for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
     const int64_t nb = a.batch - b0 < most ? a.batch - b0 : most;
-    if (ga_few(nb * per))
-      ga_fwd_kernel<D, 2, 4><<<(int)(nb * ga_halves(a.n_q) * a.q_heads), 512, 0, st>>>(ga_slice(a, b0, nb));
+    if (ga_few(a, nb * per))
+      ga_fwd_kernel<D, 2, ga_sets(D)><<<(int)(nb * ga_halves(a.n_q) * a.q_heads), 128 * ga_sets(D), 0, st>>>(ga_slice(a, b0, nb));
     else
       ga_fwd_kernel<D, 4, 1><<<(int)(nb * per), 256, 0, st>>>(ga_slice(a, b0, nb));
     const hipError_t e = hipGetLastError();
@@ -929,15 +936,15 @@ hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
   for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
     const int64_t nb = a.batch - b0 < most ? a.batch - b0 : most;
     const GroupedArgs s = ga_slice(a, b0, nb);
-    constexpr int QSETS = D == 64 ? 4 : 2;         // as many as the tiles leave LDS for
-    if (ga_few(nb * q))
-      ga_bwd_q_kernel<D, 2, QSETS><<<(int)(nb * ga_halves(a.n_q) * a.q_heads), 128 * QSETS, 0, st>>>(s);
+    if (ga_few(a, nb * q))
+      ga_bwd_q_kernel<D, 2, ga_sets(D)><<<(int)(nb * ga_halves(a.n_q) * a.q_heads), 128 * ga_sets(D), 0, st>>>(s);
     else
       ga_bwd_q_kernel<D, 4, 1><<<(int)(nb * q), 256, 0, st>>>(s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if constexpr (D == 64) {
-      if (ga_few(nb * kv))
+      // (no more blocks than CUs: 16 x 700, 8 heads over 2, no mask 106 us with 4 by 1, 96)
+      if (nb * kv <= 256)
         ga_bwd_kv_kernel<2, 4><<<(int)(nb * ga_halves(a.n_k) * a.kv_heads * a.parts), 512, 0, st>>>(s);
       else
         ga_bwd_kv_kernel<4, 1><<<(int)(nb * kv), 256, 0, st>>>(s);
