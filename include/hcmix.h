@@ -603,6 +603,8 @@ hcmix_status hcmix_grouped_attention_forward(
  *   dv = P^T dout, dS = P * (dout v^T - rowsum(dout * out)) scale,
  *   dq = dS k, dk = dS^T q, summed over the query heads of a group.
  * P is made again from lse.  Sums run in a fixed order (bitwise-repeatable).
+ * q, out and dout have to be finite in every row, those that see nothing among
+ * them (their weight of 0 meets them).
  * dk and dv are 0 from lengths[b] on.  Workspace of the size the query names
  * (0 for invalid arguments), 256-byte aligned; calls that share one must not
  * overlap; other errors as above. */
@@ -629,7 +631,9 @@ hcmix_status hcmix_grouped_attention_backward(
  * sequence b at positions[b] and behind, its first counts[b] alone (int32
  * [batch], taken within 0 .. tokens; NULL: all).  What a sequence holds from
  * positions[b] on is dropped first (so drafted tokens are taken back by
- * appending at an earlier position).  A block's scale is the larger of what its
+ * appending at an earlier position); positions[b] is no more than what it holds
+ * (tokens left out between would be undefined, and the scale of their block with
+ * them).  A block's scale is the larger of what its
  * new tokens need and, where it keeps earlier ones, its own; earlier ones are
  * then held again at the new scale.  Tokens at capacity and behind, and those of
  * a sequence whose positions[b] lies outside 0 .. capacity - 1, are left out.

@@ -1142,7 +1142,8 @@ def grouped_attention_forward(q, k, v, causal=True, lengths=None, scale=None, ou
 def grouped_attention_backward(q, k, v, out, lse, dout, causal=True, lengths=None, scale=None,
                                dq=None, dk=None, dv=None, workspace=None):
     """(dq, dk, dv) of ``grouped_attention_forward`` given its results and dout =
-    dL/dout (contiguous).  dq, dk, dv may be slices of one packed buffer."""
+    dL/dout (contiguous; finite, as q and out, in every row).  dq, dk, dv may be
+    slices of one packed buffer."""
     st = _quick(q) if workspace is None else None
     if st is not None:
         r = _marshal.grouped_backward(
@@ -1199,8 +1200,9 @@ def _cache(cache, dev):
 def kv_cache_append(k, v, positions, cache, capacity, counts=None):
     """Puts k, v [batch, tokens, kv_heads, hd] bf16 (positions may be spaced) at
     positions[b] and behind (int32 [batch] on the GPU), the first counts[b] of every
-    sequence where counts is given.  What was held from positions[b] on is
-    dropped; tokens at `capacity` and behind are left out."""
+    sequence where counts is given.  positions[b] is at most what the sequence
+    holds; what was held from there on is dropped, and tokens at `capacity` and
+    behind are left out."""
     st = _quick(k)
     if st is not None:
         r = _marshal.cache_append(_fn("hcmix_kv_cache_append"), k, v, positions, counts, cache,
