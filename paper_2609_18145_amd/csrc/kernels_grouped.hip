@@ -943,9 +943,16 @@ hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if constexpr (D == 64) {
-      // (no more blocks than CUs: 16 x 700, 8 heads over 2, no mask 106 us with 4 by 1, 96)
-      if (nb * kv <= 256)
-        ga_bwd_kv_kernel<2, 4><<<(int)(nb * ga_halves(a.n_k) * a.kv_heads * a.parts), 512, 0, st>>>(s);
+      // No more blocks of 128 keys than CUs: 64 by four sets (16 x 700, 8 heads over 2,
+      // no mask: 106 us with 4 by 1, 96), or by two where a block has few steps, so
+      // that one's beginning and end run under another's turns (64 x 256: 50.2, 44.6
+      // by two; 4 x 500: 28.0, 27.0; but 20 x 500, 64 steps: 43.5, 48.3).
+      const int halves = (int)(nb * ga_halves(a.n_k) * a.kv_heads * a.parts);
+      const int64_t steps = (int64_t)(a.n_q + GA_STEP - 1) / GA_STEP * a.group / a.parts;
+      if (nb * kv <= 256 && steps <= 32)
+        ga_bwd_kv_kernel<2, 2><<<halves, 256, 0, st>>>(s);
+      else if (nb * kv <= 256)
+        ga_bwd_kv_kernel<2, 4><<<halves, 512, 0, st>>>(s);
       else
         ga_bwd_kv_kernel<4, 1><<<(int)(nb * kv), 256, 0, st>>>(s);
     } else {
