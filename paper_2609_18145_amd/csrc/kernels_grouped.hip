@@ -504,9 +504,9 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
 // heads of 64 over 4: 980 us for the whole backward, 1008 without).
 //
 // Head dimension 64: a wave makes all four products of its 32 keys.  W and KS as in
-// the forward: where the blocks are few, two waves of keys by four sets that share
-// the query tiles (8 x 1024, 16 heads over 4: 108 us for the whole backward with
-// four by two, 94 so; 1 x 256, 8 heads 20.4, 19.3).
+// the forward: where the blocks are few, two waves of keys by four or two sets that
+// share the query tiles (8 x 1024, 16 heads over 4: 108 us for the whole backward
+// with four by two, 94 with two by four; 1 x 256, 8 heads 20.4, 19.3).
 template <int W, int KS>
 __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_kv_kernel(GroupedArgs a) {
   constexpr int D = 64, ROWS = 32 * W;
