@@ -32,6 +32,17 @@ constexpr int GA_ROWS = 128;
 template <int I>
 using Const = std::integral_constant<int, I>;
 
+// A block's waves meet, each with at most N of its copies on their way and its LDS
+// reads done.
+template <int N>
+__device__ __forceinline__ void ga_meet() {
+  static_assert(N < 16, "");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | N);       // vmcnt N, expcnt any, lgkmcnt 0
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // Fragments of a tile of R rows.
 template <int R>
 __device__ __forceinline__ bf16x8 ga_frag(const bf16* t, int r0, int c0, int lane) {
@@ -682,15 +693,22 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_kv_kernel(GroupedArgs a
 // Head dimension 128: all four products of 32 keys take more than half of a SIMD's
 // registers, and a wave that is alone there waits for itself.  So two waves of one
 // SIMD share them: the first makes S, P and dV, the second dP, dS and dK a turn
-// later, from the P in fp32 that the first leaves in LDS.  The tiles of two turns
-// back, now and the next are in use, the fourth buffer's is on its way.  (8 x 4096,
-// 8 heads over 2: the backward 970 us with a wave for all four, 909 so, 925 without
-// the hint on order; 32 x 512: 122, 113; by head dimension 64 952 and 1064: there
-// the exchange costs more LDS than it hides.)
+// later, from the P in fp32 that the first leaves in LDS.  (8 x 4096, 8 heads over
+// 2: the backward 970 us with a wave for all four, 909 so, 925 without the hint on
+// order; 32 x 512: 122, 113; by head dimension 64 952 and 1064: there the exchange
+// costs more LDS than it hides.)
+//
+// The last turn's tiles, this one's and the next are in use, the fourth buffer's are
+// on their way.  A buffer is an LDS variable of its own, so that the compiler sees
+// that no read of the turn waits for them (in one variable 8 x 4096 took 937 us on a
+// card where it is 924, 3 x 1000 70.2 and 68.0).
 __global__ __launch_bounds__(512, 2) void ga_bwd_pair_kernel(GroupedArgs a) {
   constexpr int D = 128;
-  __shared__ __attribute__((aligned(1024))) bf16 sT[GA_BUFS][2][GA_STEP * D];   // queries, dout
-  __shared__ __attribute__((aligned(1024))) float sS[GA_BUFS][256];
+  struct Tiles {
+    bf16 rows[2][GA_STEP * D];                 // queries, dout
+    float stats[256];
+  };
+  __shared__ __attribute__((aligned(1024))) Tiles t0, t1, t2, t3;
   __shared__ __attribute__((aligned(1024))) f32x4 sP[2][4][4][64];              // [turn % 2][wave][quad][lane]
   Item it;
   const int key_tiles = (a.n_k + GA_ROWS - 1) / GA_ROWS;
@@ -719,13 +737,19 @@ __global__ __launch_bounds__(512, 2) void ga_bwd_pair_kernel(GroupedArgs a) {
   const TileDma<D, GA_STEP> dma(wave, lane, stride);
   int lg = per ? lo / per : 0, lt = lo - lg * per;       // head and tile to be loaded next
   int ct = lt;                                           // tile to be computed next
+  auto tiles = [&](auto buf) -> Tiles& {
+    if constexpr (buf == 0) return t0;
+    else if constexpr (buf == 1) return t1;
+    else if constexpr (buf == 2) return t2;
+    else return t3;
+  };
   auto load = [&](auto buf, int step) {                  // buf: step % GA_BUFS
     if (step >= steps) return;
     const int h = it.h * a.group + lg, i0 = (first + lt) * GA_STEP;
-    dma.load(src + (size_t)h * D, stride, i0, a.n_q, sT[buf][role]);
+    dma.load(src + (size_t)h * D, stride, i0, a.n_q, tiles(buf).rows[role]);
     if (wave == 0 && role == 0)
       dma16_at((const bf16*)(a.stats + ga_stats(it.b * a.q_heads + h, a.n_q, i0)), 16 * (lane & 15),
-               (bf16*)sS[buf]);
+               (bf16*)tiles(buf).stats);
     if (++lt == per) {
       lt = 0;
       lg++;
@@ -734,12 +758,12 @@ __global__ __launch_bounds__(512, 2) void ga_bwd_pair_kernel(GroupedArgs a) {
   auto product = [&](auto buf, f32x16& x) {              // S or dP
 #pragma unroll
     for (int g = 0; g < 4; g++) {
-      const f32x4 y = *(const f32x4*)(sS[buf] + 32 * role + 8 * g + 4 * half);
+      const f32x4 y = *(const f32x4*)(tiles(buf).stats + 32 * role + 8 * g + 4 * half);
 #pragma unroll
       for (int r = 0; r < 4; r++) x[4 * g + r] = y[r];
     }
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ks++) x = mfma32(ga_frag<GA_STEP>(sT[buf][role], 0, 16 * ks, lane), xf[ks], x);
+    for (int ks = 0; ks < D / 16; ks++) x = mfma32(ga_frag<GA_STEP>(tiles(buf).rows[role], 0, 16 * ks, lane), xf[ks], x);
   };
   auto gather = [&](auto buf, const f32x16& x) {         // dV or dK
 #pragma unroll
@@ -747,12 +771,11 @@ __global__ __launch_bounds__(512, 2) void ga_bwd_pair_kernel(GroupedArgs a) {
       const bf16x8 f = att_pack(x, mm);
 #pragma unroll
       for (int d = 0; d < D / 32; d++)
-        acc[d] = mfma32(ga_trfrag<GA_STEP>(sT[buf][role ^ 1], 16 * mm, 32 * d, lane), f, acc[d]);
+        acc[d] = mfma32(ga_trfrag<GA_STEP>(tiles(buf).rows[role ^ 1], 16 * mm, 32 * d, lane), f, acc[d]);
     }
   };
   auto meet = [&](auto buf, int t) {
-    wait_dma();
-    __syncthreads();
+    ga_meet<0>();
     load(Const<(buf + 2) % GA_BUFS>(), t + 2);
   };
   auto turn_s = [&](auto buf, int t, f32x16& s, f32x16& next) {
@@ -791,8 +814,7 @@ __global__ __launch_bounds__(512, 2) void ga_bwd_pair_kernel(GroupedArgs a) {
   if (steps > 0) {
     load(Const<0>(), 0);
     load(Const<1>(), 1);
-    wait_dma();
-    __syncthreads();
+    ga_meet<0>();
     f32x16 x, y;
     if (role == 0) {
       product(Const<0>(), x);
