@@ -895,7 +895,7 @@ GroupedArgs ga_slice(const GroupedArgs& a, int64_t b0, int64_t nb) {
   return s;
 }
 
-constexpr int64_t GA_MAX_BLOCKS = 1 << 23;     // of a launch: below 2^32 threads
+constexpr int64_t GA_MAX_BLOCKS = 1 << 22;     // of a launch, up to 512 threads each: below 2^32
 // Whether blocks of 128 queries are so few that a CU is better given blocks of 64
 // by several sets: where they fill half of the chip, and up to all of it where a
 // causal mask leaves the longest rows to a few.  us of forward and backward with

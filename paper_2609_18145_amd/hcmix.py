@@ -1308,7 +1308,11 @@ class Rotary(torch.autograd.Function):
 class GroupedAttention(torch.autograd.Function):
     """Attention over sequences of any length as an autograd function over q, k, v.
 
-    GroupedAttention.apply(q, k, v, causal, lengths, scale) -> out"""
+    GroupedAttention.apply(q, k, v, causal, lengths, scale) -> out
+
+    Captured into a graph, forward and backward go in together, from leaves that no
+    eager pass still holds (PyTorch runs a leaf's gradient on the stream of its
+    first use)."""
 
     @staticmethod
     def forward(ctx, q, k, v, causal=True, lengths=None, scale=None):

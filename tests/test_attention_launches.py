@@ -28,7 +28,9 @@ def test_grouped_forward(launches, batch, n, heads, kv, hd):  # noqa: F811
 
 
 @pytest.mark.parametrize("batch,n,heads,kv,hd", [((1 << 24) + 5, 1, 1, 1, 64), (1, 1 << 20, 256, 8, 64),
-                                                 (1 << 16, 129, 128, 1, 64), (2, 4096, 8, 8, 128)])
+                                                 (1 << 16, 129, 128, 1, 64), (2, 4096, 8, 8, 128),
+                                                 ((1 << 20) + 5, 1, 8, 8, 128), (1 << 16, 129, 64, 64, 128),
+                                                 ((1 << 20) + 5, 1, 8, 8, 64)])
 def test_grouped_backward(launches, batch, n, heads, kv, hd):  # noqa: F811
     w, kw = heads * hd, kv * hd
     ls = launches("hcmix_grouped_attention_backward",

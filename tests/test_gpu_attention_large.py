@@ -84,3 +84,19 @@ def test_a_cache_of_eight_gigabytes():
         want, size = p @ held[1][:, h // 2], p @ np.abs(held[1][:, h // 2])
         # as the oracle's bounds; the sum of four million ones in 32 bits is off by 2^-12 at most
         assert (np.abs(out[h] - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -11) * size).all()
+
+
+def test_a_million_sequences_of_one_position():
+    """More blocks than a launch takes: a position that sees itself alone gets its value
+    back, and gives its output's gradient to it.  P is 1 to 2^-20, so 1 in bf16; dP - D is
+    off by four roundings of a sum of at most 128 products of numbers below 6."""
+    batch, heads, hd = (1 << 20) + 5, 8, 128
+    g = torch.Generator("cuda").manual_seed(2)
+    q, k, v, do = (torch.randn((batch, 1, heads, hd), generator=g, device="cuda", dtype=torch.bfloat16)
+                   .clamp_(-6, 6) for _ in range(4))
+    out, lse = hcmix.grouped_attention_forward(q, k, v)
+    assert torch.equal(out, v)
+    dq, dk, dv = hcmix.grouped_attention_backward(q, k, v, out, lse, do)
+    assert torch.equal(dv, do)
+    limit = 4 * 2.0 ** -24 * 128 * 6 * 6 * 6 * hd ** -0.5
+    assert max(dq.abs().max().item(), dk.abs().max().item()) <= limit
