@@ -3,7 +3,7 @@
 // groups of query heads, keys past a sequence's length and (causal) past the
 // query's own position left out.
 //
-// The scores of 64 keys at a time never leave the registers: the forward keeps
+// The scores of 32 keys at a time never leave the registers: the forward keeps
 // each query's running maximum m and sum l of exp(S - m) and rescales what it
 // has accumulated when m grows.  The backward makes P = exp(S - lse) again from
 // the forward's lse instead of reading it.
@@ -24,6 +24,7 @@ namespace {
 
 constexpr int GA_THREADS = 256;
 constexpr float GA_LOG2E = 1.4426950408889634f, GA_LN2 = 0.6931471805599453f;
+constexpr int GA_STEP = 32;         // rows of a streamed tile
 // Rows of a block of four waves (32 to a wave).
 constexpr int GA_ROWS = 128;
 
@@ -149,7 +150,9 @@ __device__ __forceinline__ void ga_rows(bf16x8 (&f)[D / 16], const bf16* base, s
 // by more than GA_SLACK (in log2 units; P and l then stay below 2^GA_SLACK and
 // that times the number of keys, far from any limit), so that the rescaling of
 // what has been accumulated, and the exchange of the maximum between the two
-// lanes of a query, is a rare branch.
+// lanes of a query, is a rare branch.  Tiles of 32 keys leave registers for more waves
+// than 64 (64 x 256, 8 heads of 64 over 2 17.4 us with 64, 15.5; 8 x 4096, 8 of 128
+// over 2 275, 261; 8 x 4096, 16 of 64 over 4 317, 311; 16 x 500 12.9, 13.6).
 //
 // A block is W waves of queries by KS sets that share its key tiles in turn and
 // join at the end: 4 by 1, and where the blocks are few, so that a wave alone on
@@ -161,8 +164,8 @@ constexpr float GA_SLACK = 8.f;
 
 template <int D, int W, int KS>
 __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
-  constexpr int ROWS = 32 * W, TILE = KS == 1 ? 64 : 32;       // queries of a block, keys of a tile
-  __shared__ __attribute__((aligned(1024))) bf16 sKV[KS][2][2][TILE * D];   // keys, values
+  constexpr int ROWS = 32 * W;
+  __shared__ __attribute__((aligned(1024))) bf16 sKV[KS][2][2][GA_STEP * D];   // keys, values
   Item it;
   if (!ga_item(a.batch, a.q_heads, (a.n_q + ROWS - 1) / ROWS, a.causal, &it)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
@@ -177,55 +180,47 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
   const int wave_end = a.causal ? min(len, q0 + 32 + off) : len;
   const int full_end = a.causal ? min(len, q0 + 1 + off) : len;
   // tiles of the block, of this set (tile t of it is tile t KS + set), that this wave sees
-  const int all = blk_end > 0 ? (blk_end + TILE - 1) / TILE : 0;
+  const int all = blk_end > 0 ? (blk_end + GA_STEP - 1) / GA_STEP : 0;
   const int turns = (all + KS - 1) / KS, tiles = (all - set + KS - 1) / KS;
-  const int seen = q0 < a.n_q && wave_end > 0 ? (wave_end + TILE - 1) / TILE : 0;
+  const int seen = q0 < a.n_q && wave_end > 0 ? (wave_end + GA_STEP - 1) / GA_STEP : 0;
   const int mine = (seen - set + KS - 1) / KS;
-  bf16(*sK)[TILE * D] = sKV[set][0];
-  bf16(*sV)[TILE * D] = sKV[set][1];
+  bf16(*sK)[GA_STEP * D] = sKV[set][0];
+  bf16(*sV)[GA_STEP * D] = sKV[set][1];
   bf16x8 qf[D / 16];
   ga_rows<D>(qf, qb, a.q_stride, q0, a.n_q, lane);
   f32x16 o[D / 32] = {};
   const float sc = a.scale * GA_LOG2E;
   float m = -3e38f, l = 0.f, limit = -INFINITY;      // limit: the score from which m grows
-  const TileDma<D, TILE, W> dk(wave, lane, a.k_stride), dv(wave, lane, a.v_stride);
+  const TileDma<D, GA_STEP, W> dk(wave, lane, a.k_stride), dv(wave, lane, a.v_stride);
   auto load_k = [&](int t, bf16* to) {
-    if (t < tiles) dk.load(kb, a.k_stride, (t * KS + set) * TILE, len, to);
+    if (t < tiles) dk.load(kb, a.k_stride, (t * KS + set) * GA_STEP, len, to);
   };
   auto load_v = [&](int t, bf16* to) {
-    if (t < tiles) dv.load(vb, a.v_stride, (t * KS + set) * TILE, len, to);
+    if (t < tiles) dv.load(vb, a.v_stride, (t * KS + set) * GA_STEP, len, to);
   };
-  auto scores = [&](const bf16* tk, f32x16 (&r)[TILE / 32]) {
+  auto scores = [&](const bf16* tk, f32x16& r) {
+    r = f32x16{};
 #pragma unroll
-    for (int kt = 0; kt < TILE / 32; kt++) {
-      r[kt] = f32x16{};
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ks++)
-        r[kt] = mfma32(ga_frag<TILE>(tk, 32 * kt, 16 * ks, lane), qf[ks], r[kt]);
-    }
+    for (int ks = 0; ks < D / 16; ks++) r = mfma32(ga_frag<GA_STEP>(tk, 0, 16 * ks, lane), qf[ks], r);
   };
-  auto turn = [&](auto buf, int t, f32x16 (&s)[TILE / 32], f32x16 (&next)[TILE / 32]) {   // buf: t % 2
+  auto turn = [&](auto buf, int t, f32x16& s, f32x16& next) {   // buf: t % 2
     wait_dma();
     __syncthreads();
     load_k(t + 2, sK[buf]);
     load_v(t + 1, sV[buf ^ 1]);
     if (t >= mine) return;               // wave-uniform
-    const int k0 = (t * KS + set) * TILE;
-    if (k0 + TILE > full_end) {
+    const int k0 = (t * KS + set) * GA_STEP;
+    if (k0 + GA_STEP > full_end) {
       asm volatile("; tile with keys that some query does not see");   // no selects elsewhere
-      // register e of a lane: key k0 + 32 kt + 8 (e / 4) + 4 half + e % 4
+      // register e of a lane: key k0 + 8 (e / 4) + 4 half + e % 4
       const int end = (a.causal ? min(len, q0 + (lane & 31) + 1 + off) : len) - k0 - 4 * half;
 #pragma unroll
-      for (int kt = 0; kt < TILE / 32; kt++)
-#pragma unroll
-        for (int e = 0; e < 16; e++)
-          if (32 * kt + 8 * (e >> 2) + (e & 3) >= end) s[kt][e] = -INFINITY;
+      for (int e = 0; e < 16; e++)
+        if (8 * (e >> 2) + (e & 3) >= end) s[e] = -INFINITY;
     }
-    float mx = s[0][0];
+    float mx = s[0];
 #pragma unroll
-    for (int kt = 0; kt < TILE / 32; kt++)
-#pragma unroll
-      for (int e = 0; e < 16; e++) mx = fmaxf(mx, s[kt][e]);
+    for (int e = 1; e < 16; e++) mx = fmaxf(mx, s[e]);
     if (__any(mx > limit)) {
       // of the rows whose own scores ask for it: a row's result does not depend on others
       const float top = fmaxf(mx, __shfl_xor(mx, 32)), mn = top > limit ? fmaxf(m, top * sc) : m;
@@ -241,24 +236,20 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
     scores(sK[buf ^ 1], next);
     const bf16* tv = sV[buf];
 #pragma unroll
-    for (int kt = 0; kt < TILE / 32; kt++) {
+    for (int e = 0; e < 16; e++) {
+      s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], sc, -m));
+      l += s[e];
+    }
 #pragma unroll
-      for (int e = 0; e < 16; e++) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[kt][e], sc, -m));
-        s[kt][e] = p;
-        l += p;
-      }
+    for (int mm = 0; mm < 2; mm++) {
+      const bf16x8 pf = att_pack(s, mm);
 #pragma unroll
-      for (int mm = 0; mm < 2; mm++) {
-        const bf16x8 pf = att_pack(s[kt], mm);
-#pragma unroll
-        for (int d = 0; d < D / 32; d++)
-          o[d] = mfma32(ga_trfrag<TILE>(tv, 32 * kt + 16 * mm, 32 * d, lane), pf, o[d]);
-      }
+      for (int d = 0; d < D / 32; d++)
+        o[d] = mfma32(ga_trfrag<GA_STEP>(tv, 16 * mm, 32 * d, lane), pf, o[d]);
     }
   };
   if (turns) {
-    f32x16 s[TILE / 32], next[TILE / 32];
+    f32x16 s, next;
     load_k(0, sK[0]);
     load_v(0, sV[0]);
     load_k(1, sK[1]);
@@ -332,7 +323,6 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
 // first form, over sum_j P_j, which lse's own rounding keeps from being 1; with
 // more, the rounding of out adds less than a tenth to that of dS.
 // ---------------------------------------------------------------------------
-constexpr int GA_STEP = 32;         // rows of a streamed tile
 constexpr int GA_BUFS = 4;
 
 // What the dQ kernel leaves for the other, for each head and 32 rows: 32 of
