@@ -144,9 +144,7 @@ __device__ __forceinline__ void ga_rows(bf16x8 (&f)[D / 16], const bf16* base, s
 // ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
-// A wave has 32 queries.  While the exponentials of one key tile run, the matrix
-// unit makes the scores of the next: the loop carries them (its last turn makes
-// some that nothing takes).  m grows only when a tile's largest score passes it
+// A wave has 32 queries.  m grows only when a tile's largest score passes it
 // by more than GA_SLACK (in log2 units; P and l then stay below 2^GA_SLACK and
 // that times the number of keys, far from any limit), so that the rescaling of
 // what has been accumulated, and the exchange of the maximum between the two
@@ -162,9 +160,19 @@ __device__ __forceinline__ void ga_rows(bf16x8 (&f)[D / 16], const bf16* base, s
 // 128 21.0, 21.4, 17.5; 2 x 2048 of 128 34.8, 32.0, 29.8.
 constexpr float GA_SLACK = 8.f;
 
+// Whether the loops of the forward and of dQ carry the next tile's products, which the
+// matrix unit makes while the vector unit works on this one's (the last turn makes
+// some that nothing takes).  With head dimension 64 the registers that this takes are
+// better spent on a fourth wave of a SIMD, which hides the same: us of forward and
+// backward with the products ahead, and so, 8 heads over 2: 64 x 256 15.4 + 44.7,
+// 14.5 + 41.7; 300 x 64 16.5 + 45.8, 15.2 + 42.0; 8 x 4096, 16 over 4 303 + 936, the
+// same.  128: 8 x 4096 252 + 892, 256 + 910 without.
+constexpr bool ga_ahead(int D) { return D == 128; }
+
 template <int D, int W, int KS>
 __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
   constexpr int ROWS = 32 * W;
+  constexpr bool AHEAD = ga_ahead(D);
   __shared__ __attribute__((aligned(1024))) bf16 sKV[KS][2][2][GA_STEP * D];   // keys, values
   Item it;
   if (!ga_item(a.batch, a.q_heads, (a.n_q + ROWS - 1) / ROWS, a.causal, &it)) return;
@@ -206,9 +214,10 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
   auto turn = [&](auto buf, int t, f32x16& s, f32x16& next) {   // buf: t % 2
     wait_dma();
     __syncthreads();
-    load_k(t + 2, sK[buf]);
+    load_k(t + 1 + AHEAD, sK[AHEAD ? buf : buf ^ 1]);
     load_v(t + 1, sV[buf ^ 1]);
     if (t >= mine) return;               // wave-uniform
+    if constexpr (!AHEAD) scores(sK[buf], s);
     const int k0 = (t * KS + set) * GA_STEP;
     if (k0 + GA_STEP > full_end) {
       asm volatile("; tile with keys that some query does not see");   // no selects elsewhere
@@ -233,7 +242,7 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; e++) o[d][e] *= alpha;
     }
-    scores(sK[buf ^ 1], next);
+    if constexpr (AHEAD) scores(sK[buf ^ 1], next);
     const bf16* tv = sV[buf];
 #pragma unroll
     for (int e = 0; e < 16; e++) {
@@ -252,10 +261,12 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
     f32x16 s, next;
     load_k(0, sK[0]);
     load_v(0, sV[0]);
-    load_k(1, sK[1]);
-    wait_dma();
-    __syncthreads();
-    scores(sK[0], s);
+    if constexpr (AHEAD) {
+      load_k(1, sK[1]);
+      wait_dma();
+      __syncthreads();
+      scores(sK[0], s);
+    }
     for (int t = 0; t < turns; t += 2) {
       turn(Const<0>(), t, s, next);
       if (t + 1 < turns) turn(Const<1>(), t + 1, next, s);
@@ -309,8 +320,8 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
 // Backward, in two kernels: dQ by query tiles, dK and dV by key tiles, each
 // making S and dP again (7 products of the 5 that one would need with atomics on
 // dQ, whose order changes results).  Both stream tiles of 32 rows through four
-// buffers in LDS, three ahead, and carry the next tile's S and dP while the
-// vector unit works on this one's.
+// buffers in LDS, three ahead; dK and dV, and dQ where ga_ahead says so, carry the
+// next tile's S and dP while the vector unit works on this one's.
 //
 // With lanes and registers as in the forward, P = exp2((S - lse / scale) scale
 // log2 e); a row that sees nothing takes -inf for -lse: its P is 0.
@@ -334,6 +345,7 @@ __device__ __forceinline__ size_t ga_stats(int bh, int n_q, int row0) {
 template <int D, int W, int KS>
 __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a) {
   constexpr int ROWS = 32 * W;
+  constexpr bool AHEAD = ga_ahead(D);
   __shared__ __attribute__((aligned(1024))) bf16 sKV[KS][2][GA_BUFS][GA_STEP * D];   // keys, values
   Item it;
   if (!ga_item(a.batch, a.q_heads, (a.n_q + ROWS - 1) / ROWS, a.causal, &it)) return;
@@ -436,13 +448,14 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
     __syncthreads();
     if (t) load(Const<(buf + 3) % GA_BUFS>(), t + 3);
     if (t >= mine) return;                // wave-uniform
+    if constexpr (!AHEAD) scores(buf, s, dp);
     if ((t * KS + set + 1) * GA_STEP > full_end) {
       asm volatile("; tile with keys that some query does not see");   // no selects elsewhere
 #pragma unroll
       for (int e = 0; e < 16; e++)
         if ((t * KS + set) * GA_STEP + 8 * (e >> 2) + 4 * half + (e & 3) >= seen) s[e] = -INFINITY;
     }
-    scores(Const<(buf + 1) % GA_BUFS>(), s_next, dp_next);
+    if constexpr (AHEAD) scores(Const<(buf + 1) % GA_BUFS>(), s_next, dp_next);
 #pragma unroll
     for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], sc, start)) * (dp[e] - d);
     const bf16* tk = sK[buf];
@@ -456,7 +469,7 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
   };
   if (turns) {
     f32x16 s, dp, s2, dp2;
-    scores(Const<0>(), s, dp);
+    if constexpr (AHEAD) scores(Const<0>(), s, dp);
     for (int t = 0; t < turns; t += 4) {
       turn(Const<0>(), t, s, dp, s2, dp2);
       if (t + 1 < turns) turn(Const<1>(), t + 1, s2, dp2, s, dp);
