@@ -144,9 +144,13 @@ hipError_t launch_rotary(RotaryArgs a, int layout_half, int elem_bytes, hipStrea
   a.all_magic = ((1ull << 44) + all - 1) / all;
   // Rows to a block: more share the wait for the angles, fewer leave more blocks
   // to hide it: 8 x 4096 positions, 20 heads of 64 (168 MB): 36.9 us with 16 and 8,
-  // 34.0 with 4 (4.9 TB/s; a copy of as much takes 33.7).
+  // 34.0 with 4 (4.9 TB/s; a copy of as much takes 33.7).  With few heads more, up
+  // to a unit for every thread: 64 x 2048, 2 heads of 64 31.0 us with 4, 20.5; 4 heads
+  // 40.2, 29.0; 2 of 20, by single values, 29.7, 16.6.
   int rpb = 1;
-  while (rpb < 4 && rpb * (a.rot / 2) < ROT_THREADS && a.rows / (2 * rpb) >= 1024) rpb *= 2;
+  while (rpb < 16 && (rpb < 4 || rpb * all < ROT_THREADS) && rpb * (a.rot / 2) < ROT_THREADS &&
+         a.rows / (2 * rpb) >= 1024)
+    rpb *= 2;
   a.rows_per_block = rpb;
   const int64_t blocks = (a.rows + rpb - 1) / rpb;
   const int grid = blocks < (1 << 20) ? (int)blocks : 1 << 20;

@@ -39,7 +39,7 @@ def check(y, x, positions, freqs, half, scale, inverse):
 # batch, n, heads, heads beside them in the packed rows, head_dim, rot_dim
 SHAPES = [(1, 1, 1, 0, 64, 64), (64, 1, 16, 8, 64, 64), (2, 37, 5, 1, 128, 96), (3, 5, 3, 0, 80, 48),
           (2, 9, 2, 1, 34, 34), (1, 3, 7, 2, 10, 6), (2, 1030, 4, 0, 64, 32), (5, 7, 1, 0, 512, 512),
-          (1, 2, 1024, 0, 2, 2), (1, 17, 3, 0, 64, 2)]
+          (1, 2, 1024, 0, 2, 2), (1, 17, 3, 0, 64, 2), (16, 1030, 2, 1, 20, 10), (5, 4001, 1, 2, 64, 24)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -77,13 +77,13 @@ def test_scaled_contexts(scaling):
     check(y, x, pos.numpy(), freqs, True, scale, False)
 
 
-def test_more_rows_than_a_grid_has_blocks():
-    """4.2 million positions: blocks that take rows more than once; the last ones."""
-    n = (1 << 22) + 7
+@pytest.mark.parametrize("n", [(1 << 22) + 7, (1 << 24) + 7])
+def test_more_rows_than_a_grid_has_blocks(n):
+    """Millions of positions: blocks that take rows more than once; the last ones."""
     x = torch.randn((1, n, 1, 2), generator=torch.Generator("cuda").manual_seed(1), device="cuda")
     freqs, _ = hcmix.rotary_frequencies(2)
     y = hcmix.rotary(x, freqs)
-    at = torch.tensor([0, 3, 4, 12345, (1 << 22) - 1, 1 << 22, n - 1], device="cuda")
+    at = torch.tensor([0, 3, 4, 12345, n - 9, n - 8, n - 7, n - 1], device="cuda")
     check(y[:, at], x[:, at], at.cpu().numpy()[None], freqs, True, 1.0, False)
 
 
