@@ -900,13 +900,17 @@ GroupedArgs ga_slice(const GroupedArgs& a, int64_t b0, int64_t nb) {
 
 constexpr int64_t GA_MAX_BLOCKS = 1 << 22;     // of a launch, up to 512 threads each: below 2^32
 // Whether blocks of 128 queries are so few that a CU is better given blocks of 64
-// by several sets: where they fill half of the chip, and up to all of it where a
-// causal mask leaves the longest rows to a few.  us of forward and backward with
-// blocks of 128, and so, 8 heads over 2: 1 x 2048 of 64 27.7 + 68.6, 17.2 + 52.5;
-// 2 x 2048 of 128 40.0 + 127, 30.4 + 121; but 16 x 256 of 64 7.8 + 28.5,
-// 9.3 + 34.0 and 4 x 1000 of 128 without mask 23.3 + 85.7, 24.0 + 96.3.
+// by several sets: where they fill half of the chip, up to all of it where a causal
+// mask leaves the longest rows to a few, and up to two rounds where a block's few
+// rows leave half of its waves idle over a long way of keys.  us of forward and
+// backward with blocks of 128, and so, 8 heads over 2: 1 x 2048 of 64 27.7 + 68.6,
+// 17.2 + 52.5; 2 x 2048 of 128 40.0 + 127, 30.4 + 121; 64 x 64 queries of 2000 keys of
+// 64 39.9 + 101, 26.8 + 97.8; 44 x 6 of 2928, 3 heads 52.2 + 91.3, 24.3 + 62.3; but
+// 16 x 256 of 64 7.8 + 28.5, 9.3 + 34.0; 4 x 1000 of 128 without mask 23.3 + 85.7,
+// 24.0 + 96.3; 256 x 1 of 1000 42.6 + 116, 44.6 + 151; 35 x 3 of 237 of 128, 8 over 4
+// 9.5 + 28.3, 7.8 + 34.6.
 bool ga_few(const GroupedArgs& a, int64_t blocks) {
-  return blocks <= (a.causal && a.n_q >= 768 ? 256 : 128);
+  return blocks <= (a.causal && a.n_q >= 768 ? 256 : a.n_q <= 64 && a.n_k >= 1024 ? 512 : 128);
 }
 // As many sets as the tiles leave LDS for, two blocks to a CU with head dimension 128.
 constexpr int ga_sets(int D) { return D == 64 ? 4 : 2; }

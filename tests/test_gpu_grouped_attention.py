@@ -91,6 +91,8 @@ def spread(batch, n):
 MANY = [
     (70, 130, 260, 4, 2, 64, True, spread(70, 260), 1.0), (70, 260, 130, 4, 2, 128, False, spread(70, 130), 1.0),
     (66, 290, 300, 4, 2, 64, True, spread(66, 300), 2.0), (66, 300, 300, 4, 2, 128, True, None, 1.0),
+    # few queries of many keys, more such blocks than the GPU has CUs
+    (70, 3, 1030, 4, 2, 64, True, spread(70, 1030), 1.0), (70, 40, 1030, 4, 4, 128, False, None, 1.0),
 ]
 
 
