@@ -319,9 +319,9 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
 // ---------------------------------------------------------------------------
 // Backward, in two kernels: dQ by query tiles, dK and dV by key tiles, each
 // making S and dP again (7 products of the 5 that one would need with atomics on
-// dQ, whose order changes results).  Both stream tiles of 32 rows through four
-// buffers in LDS, three ahead; dK and dV, and dQ where ga_ahead says so, carry the
-// next tile's S and dP while the vector unit works on this one's.
+// dQ, whose order changes results).  Both stream tiles of 32 rows through up to four
+// buffers in LDS; dK and dV, and dQ of head dimension 128, carry the next tile's S
+// and dP while the vector unit works on this one's.
 //
 // With lanes and registers as in the forward, P = exp2((S - lse / scale) scale
 // log2 e); a row that sees nothing takes -inf for -lse: its P is 0.
@@ -330,9 +330,9 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
 // but out is rounded to bf16, and dS = P (dP - D) cancels the more the fewer keys
 // share a row: a row that sees one key has dS = 0, and got 2^-9 |dout| |out|
 // instead (dq and dk of windows of 10 keys were 0.0046 off in all, 0.0024 so).
-// So blocks whose rows see no more keys than the four buffers hold, 128, take the
-// first form, over sum_j P_j, which lse's own rounding keeps from being 1; with
-// more, the rounding of out adds less than a tenth to that of dS.
+// So blocks whose rows see no more than 128 keys, which the buffers of all sets hold
+// at once, take the first form, over sum_j P_j, which lse's own rounding keeps from
+// being 1; with more, the rounding of out adds less than a tenth to that of dS.
 // ---------------------------------------------------------------------------
 constexpr int GA_BUFS = 4;
 
@@ -345,8 +345,13 @@ __device__ __forceinline__ size_t ga_stats(int bh, int n_q, int row0) {
 template <int D, int W, int KS>
 __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a) {
   constexpr int ROWS = 32 * W;
-  constexpr bool AHEAD = ga_ahead(D);
-  __shared__ __attribute__((aligned(1024))) bf16 sKV[KS][2][GA_BUFS][GA_STEP * D];   // keys, values
+  // Sets of waves on one SIMD hide what products ahead do: then two buffers are enough,
+  // and the LDS of the others is a second block's (8 heads of 128 over 2: 3 x 1000 71.2
+  // us for the whole backward with four and products ahead, 67.8 so; 1 x 4096, 8 over 4
+  // 204, 197; of 64: 2 x 2048 68.8, 64.4).
+  constexpr bool AHEAD = ga_ahead(D) && KS == 1;
+  constexpr int BUFS = KS == 1 ? GA_BUFS : 2;
+  __shared__ __attribute__((aligned(1024))) bf16 sKV[KS][2][BUFS][GA_STEP * D];   // keys, values
   Item it;
   if (!ga_item(a.batch, a.q_heads, (a.n_q + ROWS - 1) / ROWS, a.causal, &it)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
@@ -367,15 +372,17 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
   bf16(*sK)[GA_STEP * D] = sKV[set][0];
   bf16(*sV)[GA_STEP * D] = sKV[set][1];
   const TileDma<D, GA_STEP, W> dk(wave, lane, a.k_stride), dv(wave, lane, a.v_stride);
-  auto load = [&](auto buf, int t) {      // buf: t % GA_BUFS
+  auto load = [&](auto buf, int t) {      // buf: t % BUFS
     if (t >= tiles) return;
     dk.load(kb, a.k_stride, (t * KS + set) * GA_STEP, len, sK[buf]);
     dv.load(vb, a.v_stride, (t * KS + set) * GA_STEP, len, sV[buf]);
   };
   load(Const<0>(), 0);
   load(Const<1>(), 1);
-  load(Const<2>(), 2);
-  load(Const<3>(), 3);
+  if constexpr (BUFS == 4) {
+    load(Const<2>(), 2);
+    load(Const<3>(), 3);
+  }
   bf16x8 qf[D / 16], of[D / 16];
   ga_rows<D>(qf, a.q + (size_t)it.b * a.n_q * a.q_stride + (size_t)it.h * D, a.q_stride, q0, a.n_q, lane);
   ga_rows<D>(of, a.dout + (size_t)it.b * a.n_q * os + (size_t)it.h * D, os, q0, a.n_q, lane);
@@ -443,10 +450,10 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
   };
   auto turn = [&](auto buf, int t, f32x16& s, f32x16& dp, f32x16& s_next, f32x16& dp_next) {
     // tile t + 1 has landed when at most t + 2's loads are on their way
-    if (t + 2 < tiles) wait_vmcnt<2 * TileDma<D, GA_STEP, W>::PER>();
+    if (BUFS == 4 && t + 2 < tiles) wait_vmcnt<2 * TileDma<D, GA_STEP, W>::PER>();
     else wait_vmcnt<0>();
     __syncthreads();
-    if (t) load(Const<(buf + 3) % GA_BUFS>(), t + 3);
+    if (t) load(Const<(buf + BUFS - 1) % BUFS>(), t + BUFS - 1);
     if (t >= mine) return;                // wave-uniform
     if constexpr (!AHEAD) scores(buf, s, dp);
     if ((t * KS + set + 1) * GA_STEP > full_end) {
@@ -455,7 +462,7 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
       for (int e = 0; e < 16; e++)
         if ((t * KS + set) * GA_STEP + 8 * (e >> 2) + 4 * half + (e & 3) >= seen) s[e] = -INFINITY;
     }
-    if constexpr (AHEAD) scores(Const<(buf + 1) % GA_BUFS>(), s_next, dp_next);
+    if constexpr (AHEAD) scores(Const<(buf + 1) % BUFS>(), s_next, dp_next);
 #pragma unroll
     for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], sc, start)) * (dp[e] - d);
     const bf16* tk = sK[buf];
@@ -470,11 +477,13 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
   if (turns) {
     f32x16 s, dp, s2, dp2;
     if constexpr (AHEAD) scores(Const<0>(), s, dp);
-    for (int t = 0; t < turns; t += 4) {
+    for (int t = 0; t < turns; t += BUFS) {
       turn(Const<0>(), t, s, dp, s2, dp2);
       if (t + 1 < turns) turn(Const<1>(), t + 1, s2, dp2, s, dp);
-      if (t + 2 < turns) turn(Const<2>(), t + 2, s, dp, s2, dp2);
-      if (t + 3 < turns) turn(Const<3>(), t + 3, s2, dp2, s, dp);
+      if constexpr (BUFS == 4) {
+        if (t + 2 < turns) turn(Const<2>(), t + 2, s, dp, s2, dp2);
+        if (t + 3 < turns) turn(Const<3>(), t + 3, s2, dp2, s, dp);
+      }
     }
   }
   if constexpr (KS > 1) {                 // as in the forward
