@@ -54,6 +54,20 @@ __device__ __forceinline__ bf16x8 ga_trfrag(const bf16* t, int k0, int c0, int l
   return att_trfrag(t + (c0 >> 6) * R * HD, k0, c0 & 63, lane);
 }
 
+// What att_pack's rounding leaves of those registers, rounded in its turn.  In a call
+// of few scores the roundings of P and dS do not average out: of 1024 and fewer, dq
+// and dk were up to 1.5 to 2.8 times as far off as their own rounding to bf16 leaves
+// them, 1.42 in the mean; from 131072 on 1.45 at most.  Such a call waits for
+// latencies, so that the FINE kernels' second products with what is left cost it
+// little (1 x 128, 2 heads of 64: 5.2 + 14.1 us, 5.4 + 16.5), and its results are as
+// near as their own rounding.
+__device__ __forceinline__ bf16x8 ga_rest(const f32x16& s, int m) {
+  bf16x8 v;
+#pragma unroll
+  for (int e = 0; e < 8; e++) v[e] = to_bf16(s[8 * m + e] - (float)to_bf16(s[8 * m + e]));
+  return v;
+}
+
 // A tile's way straight into LDS: rows row0 .. + R of an array with rows `stride`
 // elements apart; rows at `valid` and behind are copies of the last before it
 // (finite where the valid ones are: their P is 0).  A wave copies every W-th piece
@@ -169,7 +183,7 @@ constexpr float GA_SLACK = 8.f;
 // same.  128: 8 x 4096 252 + 892, 256 + 910 without.
 constexpr bool ga_ahead(int D) { return D == 128; }
 
-template <int D, int W, int KS>
+template <int D, int W, int KS, bool FINE = false>
 __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
   constexpr int ROWS = 32 * W;
   constexpr bool AHEAD = ga_ahead(D);
@@ -255,6 +269,15 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
 #pragma unroll
       for (int d = 0; d < D / 32; d++)
         o[d] = mfma32(ga_trfrag<GA_STEP>(tv, 16 * mm, 32 * d, lane), pf, o[d]);
+    }
+    if constexpr (FINE) {
+#pragma unroll
+      for (int mm = 0; mm < 2; mm++) {
+        const bf16x8 pf = ga_rest(s, mm);
+#pragma unroll
+        for (int d = 0; d < D / 32; d++)
+          o[d] = mfma32(ga_trfrag<GA_STEP>(tv, 16 * mm, 32 * d, lane), pf, o[d]);
+      }
     }
   };
   if (turns) {
@@ -342,7 +365,7 @@ __device__ __forceinline__ size_t ga_stats(int bh, int n_q, int row0) {
   return ((size_t)bh * ((n_q + 31) / 32) + row0 / 32) * 64;
 }
 
-template <int D, int W, int KS>
+template <int D, int W, int KS, bool FINE = false>
 __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a) {
   constexpr int ROWS = 32 * W;
   // Sets of waves on one SIMD hide what products ahead do: then two buffers are enough,
@@ -473,6 +496,15 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
       for (int dt = 0; dt < D / 32; dt++)
         gq[dt] = mfma32(ga_trfrag<GA_STEP>(tk, 16 * mm, 32 * dt, lane), sf, gq[dt]);
     }
+    if constexpr (FINE) {
+#pragma unroll
+      for (int mm = 0; mm < 2; mm++) {
+        const bf16x8 sf = ga_rest(s, mm);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; dt++)
+          gq[dt] = mfma32(ga_trfrag<GA_STEP>(tk, 16 * mm, 32 * dt, lane), sf, gq[dt]);
+      }
+    }
   };
   if (turns) {
     f32x16 s, dp, s2, dp2;
@@ -530,7 +562,7 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
 // the forward: where the blocks are few, two waves of keys by four or two sets that
 // share the query tiles (8 x 1024, 16 heads over 4: 108 us for the whole backward
 // with four by two, 94 with two by four; 1 x 256, 8 heads 20.4, 19.3).
-template <int W, int KS>
+template <int W, int KS, bool FINE = false>
 __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_kv_kernel(GroupedArgs a) {
   constexpr int D = 64, ROWS = 32 * W;
   __shared__ __attribute__((aligned(1024))) bf16 sQO[KS][2][GA_BUFS][GA_STEP * D];   // queries, dout
@@ -632,6 +664,17 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_kv_kernel(GroupedArgs a
         dk[d] = mfma32(ga_trfrag<GA_STEP>(tq, 16 * mm, 32 * d, lane), sf, dk[d]);
       }
     }
+    if constexpr (FINE) {
+#pragma unroll
+      for (int mm = 0; mm < 2; mm++) {
+        const bf16x8 pf = ga_rest(s, mm), sf = ga_rest(dp, mm);
+#pragma unroll
+        for (int d = 0; d < D / 32; d++) {
+          dv[d] = mfma32(ga_trfrag<GA_STEP>(to, 16 * mm, 32 * d, lane), pf, dv[d]);
+          dk[d] = mfma32(ga_trfrag<GA_STEP>(tq, 16 * mm, 32 * d, lane), sf, dk[d]);
+        }
+      }
+    }
   };
   if (turns > 0) {
     f32x16 s, dp, s2, dp2;
@@ -714,6 +757,7 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_kv_kernel(GroupedArgs a
 // on their way.  A buffer is an LDS variable of its own, so that the compiler sees
 // that no read of the turn waits for them (in one variable 8 x 4096 took 937 us on a
 // card where it is 924, 3 x 1000 70.2 and 68.0).
+template <bool FINE>
 __global__ __launch_bounds__(512, 2) void ga_bwd_pair_kernel(GroupedArgs a) {
   constexpr int D = 128;
   struct Tiles {
@@ -780,10 +824,13 @@ __global__ __launch_bounds__(512, 2) void ga_bwd_pair_kernel(GroupedArgs a) {
   auto gather = [&](auto buf, const f32x16& x) {         // dV or dK
 #pragma unroll
     for (int mm = 0; mm < 2; mm++) {
-      const bf16x8 f = att_pack(x, mm);
+      const bf16x8 f = att_pack(x, mm), rest = FINE ? ga_rest(x, mm) : f;
 #pragma unroll
-      for (int d = 0; d < D / 32; d++)
-        acc[d] = mfma32(ga_trfrag<GA_STEP>(tiles(buf).rows[role ^ 1], 16 * mm, 32 * d, lane), f, acc[d]);
+      for (int d = 0; d < D / 32; d++) {
+        const bf16x8 t = ga_trfrag<GA_STEP>(tiles(buf).rows[role ^ 1], 16 * mm, 32 * d, lane);
+        acc[d] = mfma32(t, f, acc[d]);
+        if constexpr (FINE) acc[d] = mfma32(t, rest, acc[d]);
+      }
     }
   };
   auto meet = [&](auto buf, int t) {
@@ -923,6 +970,12 @@ bool ga_few(const GroupedArgs& a, int64_t blocks) {
 }
 // As many sets as the tiles leave LDS for, two blocks to a CU with head dimension 128.
 constexpr int ga_sets(int D) { return D == 64 ? 4 : 2; }
+// Whether the scores of a call are so few that their roundings do not average
+// (ga_rest); the blocks of four waves by one set, which many short sequences take,
+// leave it.
+bool ga_fine(const GroupedArgs& a) {
+  return (int64_t)a.batch * a.q_heads * a.n_q <= (1 << 16) / a.n_k;
+}
 int64_t ga_tiles(int n) { return (n + GA_ROWS - 1) / GA_ROWS; }
 int64_t ga_halves(int n) { return (n + GA_ROWS / 2 - 1) / (GA_ROWS / 2); }
 
@@ -932,10 +985,14 @@ hipError_t ga_forward(const GroupedArgs& a, hipStream_t st) {
   const int64_t most = GA_MAX_BLOCKS / per > 0 ? GA_MAX_BLOCKS / per : 1;
   for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
     const int64_t nb = a.batch - b0 < most ? a.batch - b0 : most;
-    if (ga_few(a, nb * per))
-      ga_fwd_kernel<D, 2, ga_sets(D)><<<(int)(nb * ga_halves(a.n_q) * a.q_heads), 128 * ga_sets(D), 0, st>>>(ga_slice(a, b0, nb));
+    const int halves = (int)(nb * ga_halves(a.n_q) * a.q_heads), few = 128 * ga_sets(D);
+    const GroupedArgs s = ga_slice(a, b0, nb);
+    if (!ga_few(a, nb * per))
+      ga_fwd_kernel<D, 4, 1><<<(int)(nb * per), 256, 0, st>>>(s);
+    else if (ga_fine(a))
+      ga_fwd_kernel<D, 2, ga_sets(D), true><<<halves, few, 0, st>>>(s);
     else
-      ga_fwd_kernel<D, 4, 1><<<(int)(nb * per), 256, 0, st>>>(ga_slice(a, b0, nb));
+      ga_fwd_kernel<D, 2, ga_sets(D)><<<halves, few, 0, st>>>(s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -974,10 +1031,14 @@ hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
   for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
     const int64_t nb = a.batch - b0 < most ? a.batch - b0 : most;
     const GroupedArgs s = ga_slice(a, b0, nb);
-    if (ga_few(a, nb * q))
-      ga_bwd_q_kernel<D, 2, ga_sets(D)><<<(int)(nb * ga_halves(a.n_q) * a.q_heads), 128 * ga_sets(D), 0, st>>>(s);
-    else
+    const int q_halves = (int)(nb * ga_halves(a.n_q) * a.q_heads), few = 128 * ga_sets(D);
+    const bool fine = ga_fine(a);
+    if (!ga_few(a, nb * q))
       ga_bwd_q_kernel<D, 4, 1><<<(int)(nb * q), 256, 0, st>>>(s);
+    else if (fine)
+      ga_bwd_q_kernel<D, 2, ga_sets(D), true><<<q_halves, few, 0, st>>>(s);
+    else
+      ga_bwd_q_kernel<D, 2, ga_sets(D)><<<q_halves, few, 0, st>>>(s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if constexpr (D == 64) {
@@ -987,14 +1048,19 @@ hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
       // by two; 4 x 500: 28.0, 27.0; but 20 x 500, 64 steps: 43.5, 48.3).
       const int halves = (int)(nb * ga_halves(a.n_k) * a.kv_heads * a.parts);
       const int64_t steps = (int64_t)(a.n_q + GA_STEP - 1) / GA_STEP * a.group / a.parts;
-      if (nb * kv <= 256 && steps <= 32)
-        ga_bwd_kv_kernel<2, 2><<<halves, 256, 0, st>>>(s);
-      else if (nb * kv <= 256)
-        ga_bwd_kv_kernel<2, 4><<<halves, 512, 0, st>>>(s);
-      else
+      if (nb * kv > 256)
         ga_bwd_kv_kernel<4, 1><<<(int)(nb * kv), 256, 0, st>>>(s);
+      else if (fine)
+        ga_bwd_kv_kernel<2, 2, true><<<halves, 256, 0, st>>>(s);
+      else if (steps <= 32)
+        ga_bwd_kv_kernel<2, 2><<<halves, 256, 0, st>>>(s);
+      else
+        ga_bwd_kv_kernel<2, 4><<<halves, 512, 0, st>>>(s);
     } else {
-      ga_bwd_pair_kernel<<<(int)(nb * kv), 512, 0, st>>>(s);
+      if (fine)
+        ga_bwd_pair_kernel<true><<<(int)(nb * kv), 512, 0, st>>>(s);
+      else
+        ga_bwd_pair_kernel<false><<<(int)(nb * kv), 512, 0, st>>>(s);
     }
     e = hipGetLastError();
     if (e != hipSuccess) return e;
