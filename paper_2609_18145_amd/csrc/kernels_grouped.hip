@@ -955,6 +955,16 @@ GroupedArgs ga_slice(const GroupedArgs& a, int64_t b0, int64_t nb) {
 }
 
 constexpr int64_t GA_MAX_BLOCKS = 1 << 22;     // of a launch, up to 512 threads each: below 2^32
+
+// Whether the scores of a call are so few that their roundings do not average
+// (ga_rest).  Such calls are given the form for few blocks, up to so many of them:
+// it costs 100 x 8 positions, 2 heads of 64 3.8 + 9.7 us, 5.2 + 10.7 so, but 512 x 4
+// 5.7 + 15.4, 10.6 + 28.0, and so many sequences' roundings nearly average.
+constexpr int64_t GA_FINE_BLOCKS = 256;
+bool ga_fine(const GroupedArgs& a) {
+  return (int64_t)a.batch * a.q_heads * a.n_q <= (1 << 16) / a.n_k;
+}
+
 // Whether blocks of 128 queries are so few that a CU is better given blocks of 64
 // by several sets: where they fill half of the chip, up to all of it where a causal
 // mask leaves the longest rows to a few, and up to two rounds where a block's few
@@ -966,16 +976,11 @@ constexpr int64_t GA_MAX_BLOCKS = 1 << 22;     // of a launch, up to 512 threads
 // 24.0 + 96.3; 256 x 1 of 1000 42.6 + 116, 44.6 + 151; 35 x 3 of 237 of 128, 8 over 4
 // 9.5 + 28.3, 7.8 + 34.6.
 bool ga_few(const GroupedArgs& a, int64_t blocks) {
+  if (ga_fine(a)) return blocks <= GA_FINE_BLOCKS;
   return blocks <= (a.causal && a.n_q >= 768 ? 256 : a.n_q <= 64 && a.n_k >= 1024 ? 512 : 128);
 }
 // As many sets as the tiles leave LDS for, two blocks to a CU with head dimension 128.
 constexpr int ga_sets(int D) { return D == 64 ? 4 : 2; }
-// Whether the scores of a call are so few that their roundings do not average
-// (ga_rest); the blocks of four waves by one set, which many short sequences take,
-// leave it.
-bool ga_fine(const GroupedArgs& a) {
-  return (int64_t)a.batch * a.q_heads * a.n_q <= (1 << 16) / a.n_k;
-}
 int64_t ga_tiles(int n) { return (n + GA_ROWS - 1) / GA_ROWS; }
 int64_t ga_halves(int n) { return (n + GA_ROWS / 2 - 1) / (GA_ROWS / 2); }
 
