@@ -5,7 +5,7 @@ few of them with standard multi-head attention.  An attention layer here is
 the attention core (oracle/attention.py) between two linear maps, the query /
 key / value projection and the output projection:
     qkv = x W_qkv^T   (W_qkv [3 heads head_dim][width], the rows Q, K, V in turn)
-    o   = attention(qkv)
+    o   = attention(qkv)    (in a stack that is not causal, oracle/grouped.py's without mask)
     y   = o W_out^T   (W_out [width][heads head_dim])
 with no residual, normalisation or bias, like the sparse layers (Eq. (1)).
 The schedule is a list whose entries are sparse layer codes (run by the main
@@ -19,7 +19,7 @@ from __future__ import annotations
 import numpy as np
 
 import oracle
-from oracle import attention
+from oracle import attention, grouped
 
 
 def linear_forward(x, w):
@@ -68,7 +68,8 @@ def forward(x, schedule, w_self, w_off, attn_w, heads, causal=True):
             wqkv, wout = (np.asarray(t, dtype=np.float64) for t in attn_w[arg])
             hd = wqkv.shape[0] // (3 * heads)
             qkv = linear_forward(x.reshape(-1, width), wqkv).reshape(batch, n, 3, heads, hd)
-            o, _ = attention.forward(qkv)
+            o = attention.forward(qkv)[0] if causal else grouped.forward(
+                *(qkv[:, :, i] for i in range(3)), causal=False)[0]
             o2 = o.reshape(-1, heads * hd)
             saved.append((x, qkv, o2))
             x = linear_forward(o2, wout).reshape(batch, n, -1)
@@ -96,7 +97,10 @@ def backward(saved, dy, schedule, w_self, w_off, attn_w, heads, causal=True):
             wqkv, wout = (np.asarray(t, dtype=np.float64) for t in attn_w[arg])
             hd = wqkv.shape[0] // (3 * heads)
             d_o, d_wout = linear_backward(o2, wout, g.reshape(-1, width))
-            dqkv = attention.backward(qkv, d_o.reshape(batch, n, heads, hd)).reshape(-1, 3 * heads * hd)
+            d_o = d_o.reshape(batch, n, heads, hd)
+            dqkv = attention.backward(qkv, d_o) if causal else np.stack(grouped.backward(
+                *(qkv[:, :, i] for i in range(3)), d_o, causal=False)[0], 2)
+            dqkv = dqkv.reshape(-1, 3 * heads * hd)
             g, d_wqkv = linear_backward(x.reshape(-1, width), wqkv, dqkv)
             g = g.reshape(batch, n, width)
             dattn[arg] = (d_wqkv, d_wout)

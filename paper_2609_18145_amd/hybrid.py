@@ -6,8 +6,8 @@ or hcmix.LAYER_NEAR) or "attn".  Runs of sparse layers are one hcmix stack
 each; an attention layer is the library's linear map (query/key/value
 projection), attention core and linear map (output projection); windows past
 the fixed ones (256 positions, a multiple of 32, head dimension 64), fewer
-key/value heads than query heads (kv_heads) and rotary positions take the
-attention of any length.  Backward:
+key/value heads than query heads (kv_heads) and stacks that are not causal,
+whose attention is not either, take the attention of any length.  Backward:
 each sparse run's dX chain (hcmix_stack_backward_data), each attention
 layer's three backward products, and at the end the weight gradients of all
 sparse layers in one hcmix_stack_weight_gradients call.  No arithmetic is
@@ -78,7 +78,8 @@ class HybridStack:
         hcmix.rotary(qk, positions=positions, inverse=inverse, out=qk, **self.rotary)
 
     def _fixed_window(self, n, hd):
-        return self.kv_heads == self.heads and hd == 64 and n % 32 == 0 and n <= 256
+        return (self.causal and self.kv_heads == self.heads and hd == 64 and n % 32 == 0
+                and n <= 256)
 
     # ---- one segment at a time (so that a caller can time each) ----
 
@@ -100,7 +101,7 @@ class HybridStack:
         if self._fixed_window(n, hd):
             o, lse = hcmix.attention_forward(qkv.view(batch, n, 3, self.heads, hd))
         else:
-            o, lse = hcmix.grouped_attention_forward(*self._split(packed))
+            o, lse = hcmix.grouped_attention_forward(*self._split(packed), causal=self.causal)
         y = hcmix.linear_forward(o.view(batch * n, self.heads * hd), wout)
         self._saved.append((x, qkv, o, lse))
         return y.view(batch, n, -1)
@@ -128,7 +129,7 @@ class HybridStack:
             dqkv = torch.empty_like(qkv)
             dq, dk, dv = self._split(dqkv.view(batch, n, -1, hd))
             hcmix.grouped_attention_backward(*self._split(qkv.view(batch, n, -1, hd)), o, lse, d_o,
-                                             dq=dq, dk=dk, dv=dv)
+                                             causal=self.causal, dq=dq, dk=dk, dv=dv)
         if self.rotary is not None:
             self._rotate(dqkv.view(batch, n, -1, hd), inverse=True)
         dx, d_wqkv = hcmix.linear_backward(x.view(rows, width), wqkv, dqkv.view(rows, -1))

@@ -129,3 +129,37 @@ def test_decoding_a_hybrid_follows_its_forward():
     with pytest.raises(ValueError, match="pos"):
         d.step(x[:, 0].contiguous(), n)
     assert fro_rel_err(to_host(got), y) < 0.1
+
+
+@pytest.mark.parametrize("batch,n,heads", [(2, 64, 2), (1, 512, 2)])
+def test_bidirectional_hybrid_against_the_composed_oracle(batch, n, heads):
+    """A stack that is not causal attends both ways, also over windows that the fixed
+    core takes: segment by segment, each on the library's own input and output
+    gradient, within the bf16 bound (causal attention would be off by the order of 1)."""
+    print(f"case: bidirectional hybrid {batch} {n} {heads}", flush=True)
+    width = heads * 64
+    s = inputs.make_stack(batch, n, width, 2, False, "bf16", seed=n)
+    rng = np.random.default_rng(n)
+    attn = (bf(rng, (3 * width, width), 0.25 * width ** -0.5), bf(rng, (width, width), width ** -0.5))
+    h = HybridStack([0, "attn", 1], [to_dev(a, "bf16") for a in s.w_self],
+                    [to_dev(a, "bf16") for a in s.w_off], [tuple(to_dev(a, "bf16") for a in attn)],
+                    heads, causal=False)
+    xs = [to_dev(s.x, "bf16")]
+    for k in range(3):
+        xs.append(h.forward_segment(k, xs[-1]))
+    gs = [to_dev(s.dy, "bf16")]
+    h._dw_in, h.dw_attn = [], [None]
+    for k in (2, 1, 0):
+        gs.insert(0, h.backward_segment(k, gs[0]))
+    torch.cuda.synchronize()
+    for k, segment in enumerate(h.schedule):
+        ws, wo = ([], []) if segment == "attn" else ([t[k // 2]] for t in (s.w_self, s.w_off))
+        y, saved = hybrid_oracle.forward(to_host(xs[k]), [segment], ws, wo, [attn], heads, causal=False)
+        dx, _, _, dw = hybrid_oracle.backward(saved, to_host(gs[k + 1]), [segment], ws, wo, [attn],
+                                              heads, causal=False)
+        errs = dict(y=row_rel_err(to_host(xs[k + 1]), y), dx=row_rel_err(to_host(gs[k]), dx))
+        if segment == "attn":
+            errs.update(dwqkv=fro_rel_err(to_host(h.dw_attn[0][0]), dw[0][0]),
+                        dwout=fro_rel_err(to_host(h.dw_attn[0][1]), dw[0][1]))
+        print("  ", segment, {a: f"{b:.2e}" for a, b in errs.items()}, flush=True)
+        assert max(errs.values()) <= TOL["bf16"], (segment, errs)
