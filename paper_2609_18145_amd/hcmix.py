@@ -1288,21 +1288,27 @@ def kv_cache_attention(q, lengths, cache, capacity, kv_heads, scale=None, max_le
 
 
 class Rotary(torch.autograd.Function):
-    """``rotary`` as an autograd function over x.
+    """``rotary`` as an autograd function over x, differentiable any number of times:
+    its gradient is itself by the opposite angle.
 
-    Rotary.apply(x, freqs, positions, layout, scale) -> y"""
+    Rotary.apply(x, freqs, positions, layout, scale, inverse) -> y"""
 
     @staticmethod
-    def forward(ctx, x, freqs, positions=None, layout="half", scale=1.0):
-        ctx.layout, ctx.scale = layout, scale
+    def forward(ctx, x, freqs, positions=None, layout="half", scale=1.0, inverse=False):
+        ctx.options = layout, scale, not inverse
         ctx.save_for_backward(freqs, positions)
-        return rotary(x, freqs, positions, layout, False, scale)
+        return rotary(x, freqs, positions, layout, inverse, scale)
 
     @staticmethod
     def backward(ctx, gy):
         freqs, positions = ctx.saved_tensors
-        return (rotary(gy.contiguous(), freqs, positions, ctx.layout, True, ctx.scale), None, None,
-                None, None)
+        layout, scale, inverse = ctx.options
+        gy = gy.contiguous()
+        if gy.requires_grad:             # a graph of the gradient is wanted
+            gx = Rotary.apply(gy, freqs, positions, layout, scale, inverse)
+        else:
+            gx = rotary(gy, freqs, positions, layout, inverse, scale)
+        return gx, None, None, None, None, None
 
 
 class GroupedAttention(torch.autograd.Function):

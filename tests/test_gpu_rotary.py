@@ -116,3 +116,22 @@ def test_captured_with_other_positions():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, hcmix.rotary(x, freqs, pos))
+
+
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+def test_gradient_of_a_gradient(layout):
+    """With u = R x the gradient of sum(u^3) is 3 R' u^2, and that of its product with x
+    9 R' u^2.  Values below 6 turn into u below 8.5, off by less than 12 * 2^-21 (the
+    angle's fraction 2^-22.3, products and sums 2^-24 each), u^2 by 17 times that, and
+    nine times a turn of it by sqrt(2) * 153 * 12 * 2^-21 < 2^-9; the roundings of
+    numbers below 920 on the way, 2^-24 each, stay below as much again."""
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn((2, 7, 3, 64), generator=g).clamp_(-6, 6).cuda().requires_grad_(True)
+    freqs, _ = hcmix.rotary_frequencies(64)
+    y = hcmix.Rotary.apply(x, freqs, None, layout)
+    dx, = torch.autograd.grad((y ** 3).sum(), x, create_graph=True)
+    got, = torch.autograd.grad((dx * x).sum(), x)
+    pos, half = np.arange(7)[None], layout == "half"
+    u = grouped.rotary(x.detach().cpu().numpy(), pos, freqs.cpu().numpy(), half)
+    want = 9 * grouped.rotary(u ** 2, pos, freqs.cpu().numpy(), half, inverse=True)
+    assert np.abs(got.double().cpu().numpy() - want).max() <= 2.0 ** -8

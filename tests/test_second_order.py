@@ -1,0 +1,45 @@
+"""Gradients of gradients through the attention layers' autograd functions, on the CPU:
+the library's calls are replaced by untracked ones of the same results."""
+import pytest
+import torch
+
+from paper_2609_18145_amd import hcmix
+
+f64 = torch.float64
+
+
+def rotary(x, freqs, positions=None, layout="half", inverse=False, scale=1.0, out=None):
+    """hcmix.rotary from its definition, untracked as a library call is."""
+    with torch.no_grad():
+        b, n, _, _ = x.shape
+        pos = torch.arange(n).expand(b, n) if positions is None else positions
+        t = pos.to(f64)[:, :, None, None] * freqs * (-1 if inverse else 1)
+        rot = 2 * len(freqs)
+        ia = torch.arange(rot // 2) if layout == "half" else torch.arange(0, rot, 2)
+        ib = ia + (rot // 2 if layout == "half" else 1)
+        y, a, c = x.clone(), x[..., ia], x[..., ib]
+        y[..., ia] = scale * (a * t.cos() - c * t.sin())
+        y[..., ib] = scale * (c * t.cos() + a * t.sin())
+        return y
+
+
+@pytest.mark.parametrize("layout,scale,positions", [("half", 1.0, None), ("pairs", 0.7, [[5, 900, 2], [0, 1, 7]])])
+def test_rotary_has_gradients_of_gradients(monkeypatch, layout, scale, positions):
+    monkeypatch.setattr(hcmix, "rotary", rotary)
+    freqs = hcmix.rotary_frequencies(4, device="cpu")[0]
+    pos = None if positions is None else torch.tensor(positions, dtype=torch.int32)
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn((2, 3, 2, 6), generator=g, dtype=f64).requires_grad_(True)
+
+    def turned(x):
+        return hcmix.Rotary.apply(x, freqs, pos, layout, scale)
+    assert torch.autograd.gradcheck(turned, (x,))
+    assert torch.autograd.gradgradcheck(turned, (x,))
+    # a path around the gradient as well: what was lost with no error
+    y = turned(x)
+    dx, = torch.autograd.grad((y ** 3).sum(), x, create_graph=True)
+    got, = torch.autograd.grad((dx * x).sum(), x)
+    u = rotary(x.detach(), freqs, pos, layout, scale=scale)
+    want = 9 * rotary(u ** 2, freqs, pos, layout, inverse=True, scale=scale)
+    # d/dx sum(x . R^T 3 (R x)^2) = d/dx 3 sum((R x)^3)
+    torch.testing.assert_close(got, want)
