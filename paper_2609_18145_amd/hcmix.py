@@ -31,6 +31,7 @@ import math
 import os
 
 import torch
+from torch.autograd.function import once_differentiable
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhcmix.so")
 
@@ -1316,6 +1317,7 @@ class GroupedAttention(torch.autograd.Function):
 
     GroupedAttention.apply(q, k, v, causal, lengths, scale) -> out
 
+    Differentiable once: a gradient of its gradient raises RuntimeError.
     Captured into a graph, forward and backward go in together, from leaves that no
     eager pass still holds (PyTorch runs a leaf's gradient on the stream of its
     first use)."""
@@ -1328,6 +1330,7 @@ class GroupedAttention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gout):
         q, k, v, out, lse, lengths = ctx.saved_tensors
         dq, dk, dv = grouped_attention_backward(q, k, v, out, lse, gout.contiguous(), ctx.causal,

@@ -43,3 +43,39 @@ def test_rotary_has_gradients_of_gradients(monkeypatch, layout, scale, positions
     want = 9 * rotary(u ** 2, freqs, pos, layout, inverse=True, scale=scale)
     # d/dx sum(x . R^T 3 (R x)^2) = d/dx 3 sum((R x)^3)
     torch.testing.assert_close(got, want)
+
+
+def attention(q, k, v, causal=True, lengths=None, scale=None, out=None, lse=None):
+    """hcmix.grouped_attention_forward of one key/value head per query head, untracked."""
+    with torch.no_grad():
+        s = q.shape[3] ** -0.5 * torch.matmul(q.transpose(1, 2), k.permute(0, 2, 3, 1))
+        if causal:
+            i, j = torch.arange(s.shape[2])[:, None], torch.arange(s.shape[3])
+            s = s.masked_fill(j > i + s.shape[3] - s.shape[2], float("-inf"))
+        return (s.softmax(3) @ v.transpose(1, 2)).transpose(1, 2).contiguous(), s.logsumexp(3)
+
+
+def attention_backward(q, k, v, out, lse, dout, causal=True, lengths=None, scale=None, **kw):
+    with torch.enable_grad():
+        leaves = [t.detach().requires_grad_(True) for t in (q, k, v)]
+        s = q.shape[3] ** -0.5 * torch.matmul(leaves[0].transpose(1, 2), leaves[1].permute(0, 2, 3, 1))
+        if causal:
+            i, j = torch.arange(s.shape[2])[:, None], torch.arange(s.shape[3])
+            s = s.masked_fill(j > i + s.shape[3] - s.shape[2], float("-inf"))
+        out = (s.softmax(3) @ leaves[2].transpose(1, 2)).transpose(1, 2)
+        return torch.autograd.grad(out, leaves, dout.detach())
+
+
+def test_attention_refuses_gradients_of_gradients(monkeypatch):
+    """The first order is right also with a graph of it; the second says that there is none."""
+    monkeypatch.setattr(hcmix, "grouped_attention_forward", attention)
+    monkeypatch.setattr(hcmix, "grouped_attention_backward", attention_backward)
+    g = torch.Generator().manual_seed(2)
+    q, k, v = (torch.randn((1, 3, 2, 4), generator=g, dtype=f64).requires_grad_(True) for _ in range(3))
+    assert torch.autograd.gradcheck(hcmix.GroupedAttention.apply, (q, k, v))
+    y = hcmix.GroupedAttention.apply(q, k, v)
+    dq, = torch.autograd.grad((y ** 2).sum(), q, create_graph=True)
+    want, = torch.autograd.grad((hcmix.GroupedAttention.apply(q, k, v) ** 2).sum(), q)
+    assert torch.equal(dq, want)
+    with pytest.raises(RuntimeError, match="differentiate twice"):
+        (dq * q).sum().backward()
