@@ -1339,7 +1339,7 @@ class GroupedAttention(torch.autograd.Function):
 
 
 class Attention(torch.autograd.Function):
-    """The attention core as an autograd function over qkv."""
+    """The attention core as an autograd function over qkv (differentiable once)."""
 
     @staticmethod
     def forward(ctx, qkv):
@@ -1348,6 +1348,7 @@ class Attention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gout):
         qkv, out, lse = ctx.saved_tensors
         return attention_backward(qkv, out, lse, gout.contiguous())
@@ -1393,7 +1394,7 @@ def decode_step(x, w_selfs, w_offs, layers, n, pos, cache, out=None):
 
 
 class Stack(torch.autograd.Function):
-    """Autograd over a stack of mixing layers.
+    """Autograd over a stack of mixing layers (differentiable once).
 
     Stack.apply(x, layers, causal, *w_selfs, *w_offs) -> x_L"""
 
@@ -1407,6 +1408,7 @@ class Stack(torch.autograd.Function):
         return xs[-1]
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy):
         L = len(ctx.layers)
         saved = ctx.saved_tensors

@@ -79,3 +79,42 @@ def test_attention_refuses_gradients_of_gradients(monkeypatch):
     assert torch.equal(dq, want)
     with pytest.raises(RuntimeError, match="differentiate twice"):
         (dq * q).sum().backward()
+
+
+def test_fixed_attention_refuses_gradients_of_gradients(monkeypatch):
+    def forward(qkv):
+        out, lse = attention(*qkv.unbind(2))
+        return out, lse
+
+    def backward(qkv, out, lse, dout):
+        return torch.stack(attention_backward(*qkv.unbind(2), out, lse, dout), 2)
+    monkeypatch.setattr(hcmix, "attention_forward", forward)
+    monkeypatch.setattr(hcmix, "attention_backward", backward)
+    g = torch.Generator().manual_seed(3)
+    qkv = torch.randn((1, 3, 3, 2, 4), generator=g, dtype=f64).requires_grad_(True)
+    assert torch.autograd.gradcheck(hcmix.Attention.apply, (qkv,))
+    dqkv, = torch.autograd.grad((hcmix.Attention.apply(qkv) ** 2).sum(), qkv, create_graph=True)
+    with pytest.raises(RuntimeError, match="differentiate twice"):
+        (dqkv * qkv).sum().backward()
+
+
+def test_stack_refuses_gradients_of_gradients(monkeypatch):
+    """(A stack of one map, x W' for the library's layers.)"""
+    def forward(x, w_selfs, w_offs, layers, causal):
+        with torch.no_grad():
+            return [x, x @ w_selfs[0].T]
+
+    def backward(xs, w_selfs, w_offs, layers, dy, causal):
+        with torch.no_grad():
+            dw = dy.reshape(-1, dy.shape[-1]).T @ xs[0].reshape(-1, xs[0].shape[-1])
+            return dy @ w_selfs[0], [dw], [torch.zeros_like(w_offs[0])]
+    monkeypatch.setattr(hcmix, "stack_forward", forward)
+    monkeypatch.setattr(hcmix, "stack_backward", backward)
+    g = torch.Generator().manual_seed(4)
+    x, ws, wo = (torch.randn(s, generator=g, dtype=f64).requires_grad_(True)
+                 for s in ((2, 3, 4), (4, 4), (4, 4)))
+    assert torch.autograd.gradcheck(lambda *t: hcmix.Stack.apply(t[0], [0], True, *t[1:]), (x, ws, wo))
+    y = hcmix.Stack.apply(x, [0], True, ws, wo)
+    dx, = torch.autograd.grad((y ** 3).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="differentiate twice"):
+        (dx * x).sum().backward()
