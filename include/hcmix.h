@@ -639,8 +639,9 @@ hcmix_status hcmix_grouped_attention_backward(
  * new tokens need and, where it keeps earlier ones, its own; earlier ones are
  * then held again at the new scale.  Tokens at capacity and behind, and those of
  * a sequence whose positions[b] lies outside 0 .. capacity - 1, are left out.
- * An infinity takes the scale to 2^120 and is held as 448 times it; NaN is held
- * as NaN and does not count for the scale.
+ * An infinity takes the scale to 2^120 and is held as 448 times it, which bf16 reads
+ * as infinity; finite numbers are held to 240 times it (those from 248 2^120 on, 3.3e38,
+ * would round past bf16's); NaN is held as NaN and does not count for the scale.
  *
  * Read: k and v (bf16 [batch][tokens][kv_heads][head_dim]) of tokens first[b] ..
  * first[b] + tokens - 1, the values held (exact in bf16), 0 outside 0 ..

@@ -114,6 +114,15 @@ def e4m3(x):
     return np.where(np.isnan(x), np.nan, np.sign(x) * np.round(mag / step) * step)
 
 
+def held(x, s):
+    """x as e4m3 numbers times s; at the largest scale, 2^120, finite ones are held to 240,
+    the last below 2^128."""
+    x = np.asarray(x, dtype=np.float64)
+    with np.errstate(invalid="ignore"):
+        q = x / s
+    return e4m3(np.where(np.isfinite(q), np.clip(q, -240, 240), q) if s == 2.0 ** 120 else q) * s
+
+
 def needed_scale(x):
     """The least power of two from 2^-118 to 2^120 by which |x| / 2^e <= 448."""
     mag = np.abs(x[~np.isnan(x)])
@@ -145,8 +154,7 @@ class Cache:
                 old = slice(blk * BLOCK, pos + t)
                 if pos + t > blk * BLOCK:
                     s = max(s, self.scale[blk, h])
-                    self.held[old, h] = e4m3(self.held[old, h] / s) * s
-                with np.errstate(invalid="ignore"):
-                    self.held[pos + t:pos + t + n, h] = e4m3(x[t:t + n, h] / s) * s
+                    self.held[old, h] = held(self.held[old, h], s)
+                self.held[pos + t:pos + t + n, h] = held(x[t:t + n, h], s)
                 self.scale[blk, h] = s
             t += n

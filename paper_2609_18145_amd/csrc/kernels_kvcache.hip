@@ -49,6 +49,14 @@ __device__ __forceinline__ float kv_scale(float amax) {
   return __uint_as_float((unsigned)(e + 127) << 23);
 }
 
+// At the scale 2^120 quotients reach 255, which e4m3 rounds to 256 from 248 on: 2^128,
+// infinite in bf16.  So finite numbers are held to 240 2^120.  (One past that asks for the
+// scale 2^120 by itself.)
+constexpr float KV_TOP = 0x1p120f, KV_MOST = 0x1.ep127f;
+__device__ __forceinline__ float kv_finite(float x) {
+  return x > KV_MOST && x < INFINITY ? KV_MOST : x < -KV_MOST && x > -INFINITY ? -KV_MOST : x;
+}
+
 // |v| <= 448 or infinite (held as 448), or NaN (held as NaN).
 __device__ __forceinline__ unsigned char kv_byte(float v) {
   v = v > 448.f ? 448.f : v < -448.f ? -448.f : v;
@@ -170,6 +178,13 @@ __global__ __launch_bounds__(KV_THREADS) void kv_append_kernel(KvAppendArgs a) {
       ((u32x4*)cv)[i] = kv_rescaled(((u32x4*)cv)[i], ov / sv);
     __syncthreads();                               // new bytes go between them
   }
+  if (sk == KV_TOP || sv == KV_TOP)                // of the block
+#pragma unroll
+    for (int i = 0; i < PER; i++)
+#pragma unroll
+      for (int r = 0; r < 4; r++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[i][r][e] = (bf16)kv_finite((float)x[i][r][e]);
   const float ik = 1.f / sk, iv = 1.f / sv;        // exact
 #pragma unroll
   for (int i = 0; i < PER; i++) {
@@ -235,8 +250,8 @@ __global__ __launch_bounds__(KV_THREADS) void kv_append_one_kernel(KvAppendArgs 
   float x[DL], y[DL], mk = 0.f, mv = 0.f;
 #pragma unroll
   for (int i = 0; i < DL; i++) {
-    x[i] = (float)a.k[(size_t)b * a.k_stride + (size_t)h * D + 64 * i + lane];
-    y[i] = (float)a.v[(size_t)b * a.v_stride + (size_t)h * D + 64 * i + lane];
+    x[i] = kv_finite((float)a.k[(size_t)b * a.k_stride + (size_t)h * D + 64 * i + lane]);
+    y[i] = kv_finite((float)a.v[(size_t)b * a.v_stride + (size_t)h * D + 64 * i + lane]);
     mk = fmaxf(mk, fabsf(x[i]));
     mv = fmaxf(mv, fabsf(y[i]));
   }

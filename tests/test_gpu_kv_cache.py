@@ -224,3 +224,26 @@ def test_calls_on_two_streams_at_once():
             got.append(decode(i + 1))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("chunks", [[70], [1] * 4, [3, 1, 66]])
+def test_the_largest_finite_numbers_stay_finite(chunks):
+    """From 248 2^120 on a quotient at the largest scale would round to 2^128."""
+    top = torch.finfo(torch.bfloat16).max
+    n = sum(chunks)
+    x = torch.zeros((1, n, 1, 64), dtype=torch.bfloat16, device="cuda")
+    for t, v in enumerate((top, -top, 3.31e38, 3.29e38, -3.2e38, 1e30, float("inf"))[:n]):
+        x[0, t, 0, 5 * t] = v
+    c, pos = Both(1, n, 1, 64), 0
+    for m in chunks:
+        c.append(x[:, pos:pos + m].contiguous(), -x[:, pos:pos + m].contiguous(), [pos])
+        pos += m
+    got = hcmix.kv_cache_read(c.cache, n, 1, 64, ints([0]), ints([n]), n)
+    for t, ref, sign in zip(got, c.ref, (1, -1)):
+        assert torch.equal(t.isinf(), x.isinf())
+        want = np.where(x.isinf().cpu().numpy()[0], sign * np.inf, ref[0].held)
+        np.testing.assert_array_equal(t[0].double().cpu().numpy(), want)
+    # one token alone: its value back
+    out = hcmix.kv_cache_attention(torch.zeros((1, 1, 1, 64), dtype=torch.bfloat16, device="cuda"),
+                                   ints([1]), c.cache, n, 1)
+    assert torch.equal(out, got[1][:, :1]) and out.isfinite().all()
