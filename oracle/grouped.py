@@ -79,8 +79,9 @@ def forward(q, k, v, causal=True, lengths=None, scale=None):
     return out, lse, bound
 
 
-def backward(q, k, v, dout, causal=True, lengths=None, scale=None):
-    """((dq, dk, dv), (their bounds))."""
+def backward(q, k, v, dout, causal=True, lengths=None, scale=None, exact=0):
+    """((dq, dk, dv), (their bounds)); out's rounding plays no part in rows that see at
+    most `exact` keys."""
     q, k, v, lengths, scale, group = _operands(q, k, v, lengths, scale)
     dout = np.asarray(dout, dtype=np.float64)
     g = [np.zeros_like(t) for t in (q, k, v)]
@@ -97,7 +98,7 @@ def backward(q, k, v, dout, causal=True, lengths=None, scale=None):
             g[1][b, :n, c] += scale * ds.T @ qh
             g[2][b, :n, c] += p.T @ do
             dd = np.abs(do * o).sum(axis=1)[:, None]
-            off = scale * (U * np.abs(ds) + U * p * dd
+            off = scale * (U * np.abs(ds) + U * p * dd * (seen.sum(axis=1) > exact)[:, None]
                            + F * p * (np.abs(do) @ np.abs(vh).T + dd))
             e[0][b, :, h] = off @ np.abs(kh)
             e[1][b, :n, c] += off.T @ np.abs(qh)

@@ -353,9 +353,11 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
 // but out is rounded to bf16, and dS = P (dP - D) cancels the more the fewer keys
 // share a row: a row that sees one key has dS = 0, and got 2^-9 |dout| |out|
 // instead (dq and dk of windows of 10 keys were 0.0046 off in all, 0.0024 so).
-// So blocks whose rows see no more than 128 keys, which the buffers of all sets hold
-// at once, take the first form, over sum_j P_j, which lse's own rounding keeps from
-// being 1; with more, the rounding of out adds less than a tenth to that of dS.
+// So rows that see no more than 128 keys, which the buffers of all sets hold at once,
+// take the first form, over sum_j P_j, which lse's own rounding keeps from being 1.  The
+// others take dout . out: its rounding adds nothing to see where scores are of order 1 (dq
+// of rows of 129 and more keys 0.0024 off, as of fewer), but the more the fewer keys share
+// a row's weight (0.0035 where scores are of order 3).
 // ---------------------------------------------------------------------------
 constexpr int GA_BUFS = 4;
 
@@ -412,22 +414,43 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
   const float sc = a.scale * GA_LOG2E;
   // keys that this lane's query sees, and its statistics
   const int seen = a.causal ? min(len, q0 + (lane & 31) + 1 + off) : len;
-  float start = -INFINITY, d = 0.f, z = 0.f;
+  float start = -INFINITY, d = 0.f, z = 0.f, rounded = 0.f;
+  // whether any row of the block takes D from P and dP, and any from out (block-uniform)
+  constexpr int SHORT = GA_STEP * GA_BUFS;
+  const bool from_p = (a.causal ? min(len, blk0 + 1 + off) : len) <= SHORT, from_out = all > GA_BUFS;
   bf16x8 xf[D / 16];
-  if (all > GA_BUFS) ga_rows<D>(xf, a.out + (size_t)it.b * a.n_q * os + (size_t)it.h * D, os, q0, a.n_q, lane);
+  if (from_out) ga_rows<D>(xf, a.out + (size_t)it.b * a.n_q * os + (size_t)it.h * D, os, q0, a.n_q, lane);
   if (q0 + (lane & 31) < a.n_q) {
     const float lse = a.lse[((size_t)it.b * a.q_heads + it.h) * a.n_q + q0 + (lane & 31)];
     start = lse == -INFINITY ? -INFINITY : -lse / a.scale;
   }
   wait_vmcnt<0>();
   __syncthreads();
-  if (all > GA_BUFS) {                    // block-uniform
+  __shared__ float2 sD[KS][W][64];
+  // x and y of all sets and both lanes of a query, in one order
+  auto joined = [&](float x, float y) {
+    if constexpr (KS > 1) {
+      sD[set][wave][lane] = float2{x, y};
+      __syncthreads();
+      x = y = 0.f;
+#pragma unroll
+      for (int i = 0; i < KS; i++) {
+        x += sD[i][wave][lane].x;
+        y += sD[i][wave][lane].y;
+      }
+    }
+    return float2{x + __shfl_xor(x, 32), y + __shfl_xor(y, 32)};
+  };
+  if (from_out) {
 #pragma unroll
     for (int ks = 0; ks < D / 16; ks++)
 #pragma unroll
-      for (int e = 0; e < 8; e++) d += (float)xf[ks][e] * (float)of[ks][e];
-  } else {
-    for (int t = 0; t < mine; t++) {
+      for (int e = 0; e < 8; e++) rounded += (float)xf[ks][e] * (float)of[ks][e];
+    rounded += __shfl_xor(rounded, 32);
+  }
+  if (from_p) {
+    const int held = min(mine, GA_BUFS / KS);
+    for (int t = 0; t < held; t++) {
       f32x16 s = {}, dp = {};
 #pragma unroll
       for (int ks = 0; ks < D / 16; ks++) {
@@ -442,21 +465,10 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
         z += p;
       }
     }
-    if constexpr (KS > 1) {               // all sets' shares, in one order
-      __shared__ float2 sD[KS][W][64];
-      sD[set][wave][lane] = float2{d, z};
-      __syncthreads();
-      d = z = 0.f;
-#pragma unroll
-      for (int i = 0; i < KS; i++) {
-        d += sD[i][wave][lane].x;
-        z += sD[i][wave][lane].y;
-      }
-    }
-    z += __shfl_xor(z, 32);
+    const float2 dz = joined(d, z);
+    d = dz.y > 0.f ? dz.x / dz.y : dz.x;
   }
-  d += __shfl_xor(d, 32);
-  if (z > 0.f) d /= z;
+  if (seen > SHORT) d = rounded;
   if (q0 < a.n_q && !set)
     a.stats[ga_stats(it.b * a.q_heads + it.h, a.n_q, q0) + lane] = half ? -d : start;
   start *= sc;                            // -inf stays
