@@ -355,9 +355,13 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_fwd_kernel(GroupedArgs a) {
 // instead (dq and dk of windows of 10 keys were 0.0046 off in all, 0.0024 so).
 // So rows that see no more than 128 keys, which the buffers of all sets hold at once,
 // take the first form, over sum_j P_j, which lse's own rounding keeps from being 1.  The
-// others take dout . out: its rounding adds nothing to see where scores are of order 1 (dq
-// of rows of 129 and more keys 0.0024 off, as of fewer), but the more the fewer keys share
-// a row's weight (0.0035 where scores are of order 3).
+// others take D' = dout . out.  Its rounding adds nothing to see where scores are of order
+// 1 (dq of rows of 129 and more keys 0.0024 off, as of fewer), but the more the fewer keys
+// share a row's weight (0.0035 where scores are of order 3), so that FINE calls take the
+// rest as well: D - D' = sum_j P_j (dP_j - D') / sum_j P_j, known behind the last key, and
+// dq = sum_j P_j (dP_j - D') k_j - (D - D') sum_j P_j k_j.  The last sum is a product more
+// (1 x 16 x 512, 4 heads 13.8 us for the whole backward without, 15.2; of 128 20.0, 23.4:
+// a wave to a SIMD, for its registers).
 // ---------------------------------------------------------------------------
 constexpr int GA_BUFS = 4;
 
@@ -368,7 +372,7 @@ __device__ __forceinline__ size_t ga_stats(int bh, int n_q, int row0) {
 }
 
 template <int D, int W, int KS, bool FINE = false>
-__global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a) {
+__global__ __launch_bounds__(64 * W * KS, FINE && D == 128 ? 1 : 2) void ga_bwd_q_kernel(GroupedArgs a) {
   constexpr int ROWS = 32 * W;
   // Sets of waves on one SIMD hide what products ahead do: then two buffers are enough,
   // and the LDS of the others is a second block's (8 heads of 128 over 2: 3 x 1000 71.2
@@ -472,7 +476,10 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
   if (q0 < a.n_q && !set)
     a.stats[ga_stats(it.b * a.q_heads + it.h, a.n_q, q0) + lane] = half ? -d : start;
   start *= sc;                            // -inf stays
-  f32x16 gq[D / 32] = {};
+  // FINE: sums of P (dP - D), of P, and of P K for what the first says
+  f32x16 gq[D / 32] = {}, gp[FINE ? D / 32 : 1] = {};
+  float left = 0.f;
+  z = 0.f;
   auto scores = [&](auto buf, f32x16& s, f32x16& dp) {
     const bf16 *tk = sK[buf], *tv = sV[buf];
     s = f32x16{};
@@ -499,8 +506,26 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
     }
     if constexpr (AHEAD) scores(Const<(buf + 1) % BUFS>(), s_next, dp_next);
 #pragma unroll
-    for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], sc, start)) * (dp[e] - d);
+    for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], sc, start));
     const bf16* tk = sK[buf];
+    if constexpr (FINE) {
+      if (from_out) {
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+          left = fmaf(s[e], dp[e] - d, left);
+          z += s[e];
+        }
+#pragma unroll
+        for (int mm = 0; mm < 2; mm++) {
+          const bf16x8 pf = att_pack(s, mm);
+#pragma unroll
+          for (int dt = 0; dt < D / 32; dt++)
+            gp[dt] = mfma32(ga_trfrag<GA_STEP>(tk, 16 * mm, 32 * dt, lane), pf, gp[dt]);
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 16; e++) s[e] *= dp[e] - d;
 #pragma unroll
     for (int mm = 0; mm < 2; mm++) {
       const bf16x8 sf = att_pack(s, mm);
@@ -528,6 +553,17 @@ __global__ __launch_bounds__(64 * W * KS, 2) void ga_bwd_q_kernel(GroupedArgs a)
         if (t + 2 < turns) turn(Const<2>(), t + 2, s, dp, s2, dp2);
         if (t + 3 < turns) turn(Const<3>(), t + 3, s2, dp2, s, dp);
       }
+    }
+  }
+  if constexpr (FINE) {
+    if (from_out) {
+      const float2 lz = joined(left, z);
+      const float more = seen > SHORT && lz.y > 0.f ? lz.x / lz.y : 0.f;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) gq[dt][e] -= more * gp[dt][e];
+      if (q0 < a.n_q && !set && half) a.stats[ga_stats(it.b * a.q_heads + it.h, a.n_q, q0) + lane] = -(d + more);
     }
   }
   if constexpr (KS > 1) {                 // as in the forward

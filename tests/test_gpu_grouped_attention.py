@@ -301,3 +301,26 @@ def test_rows_of_few_keys_beside_rows_of_many(case):
         err = np.linalg.norm(host(got[0])[:, rows] - r)
         print(f"  dq of rows of {lo} to {hi} keys: {err / own:.3f} of its own rounding", flush=True)
         assert err <= 1.6 * own, (lo, hi)
+
+
+@pytest.mark.parametrize("case", [(1, 16, 512, 4, 4, 64, False), (1, 16, 512, 4, 4, 128, False), (1, 100, 300, 2, 1, 64, True),
+                                  (1, 100, 300, 2, 1, 128, True), (1, 1, 4000, 8, 2, 128, True), (1, 6, 2900, 3, 1, 64, True)],
+                         ids=lambda c: "x".join(map(str, c[:6])))
+def test_few_scores_of_many_keys_are_as_near(case):
+    """As the calls of few scores above, also past 128 keys and with weights that few
+    keys share (queries of size 3)."""
+    batch, n_q, n_k, heads, kv, hd, causal = case
+    for seed in range(3):
+        q, k, v, do = draw(batch, n_q, n_k, heads, kv, hd, seed=seed, size=3.0)
+        lengths = None if seed else [n_k - 150] * batch
+        ln = None if seed else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+        out, lse = hcmix.grouped_attention_forward(q, k, v, causal, ln)
+        got = (out, *hcmix.grouped_attention_backward(q, k, v, out, lse, do, causal, ln))
+        hq, hk, hv, hdo = (host(t) for t in (q, k, v, do))
+        ref = (grouped.forward(hq, hk, hv, causal, lengths)[0],
+               *grouped.backward(hq, hk, hv, hdo, causal, lengths)[0])
+        for name, g, r in zip(("out", "dq", "dk", "dv"), got, ref):
+            own = np.linalg.norm(host(torch.from_numpy(r).to(torch.bfloat16)) - r)
+            err = np.linalg.norm(host(g) - r)
+            print(f"  {name}: {err / own:.3f} of its own rounding", flush=True)
+            assert err <= 1.05 * own, name
