@@ -586,8 +586,8 @@ hcmix_status hcmix_rotary(int64_t rows, int32_t heads, int32_t head_dim, int32_t
  *   [head_dim], lse: fp32 [batch][q_heads][n_q], both contiguous.
  * Precision: products of bf16 with fp32 accumulation, softmax statistics in fp32,
  * P (and the backward's P and dS) rounded to bf16 for the second products, or taken
- * as two bf16 numbers in a call of at most 2^16 scores (batch q_heads n_q n_k) whose
- * blocks are few.
+ * as two bf16 numbers in a call of at most 2^16 scores (batch q_heads n_q n_k) in at
+ * most 256 blocks of 128 queries of a head (batch q_heads ceil(n_q / 128)).
  * n_q, n_k <= 2^20, q_heads <= 1024, batch * n <= 2^30; scale 2^-24 .. 2^24.
  * HCMIX_ERR_INVALID_VALUE: null pointers (lengths may be), sizes < 1 or past
  * those bounds, q_heads no multiple of kv_heads, causal not 0 or 1, strides

@@ -1005,12 +1005,16 @@ GroupedArgs ga_slice(const GroupedArgs& a, int64_t b0, int64_t nb) {
 constexpr int64_t GA_MAX_BLOCKS = 1 << 22;     // of a launch, up to 512 threads each: below 2^32
 
 // Whether the scores of a call are so few that their roundings do not average
-// (ga_rest).  Such calls are given the form for few blocks, up to so many of them:
-// it costs 100 x 8 positions, 2 heads of 64 3.8 + 9.7 us, 5.2 + 10.7 so, but 512 x 4
-// 5.7 + 15.4, 10.6 + 28.0, and so many sequences' roundings nearly average.
+// (ga_rest), for all of its kernels alike.  Such calls are given the form for few blocks,
+// up to so many blocks of 128 queries: it costs 100 x 8 positions, 2 heads of 64 3.8 + 9.7
+// us, 5.2 + 10.7 so, but 512 x 4 5.7 + 15.4, 10.6 + 28.0, and so many sequences' roundings
+// nearly average.
 constexpr int64_t GA_FINE_BLOCKS = 256;
+int64_t ga_tiles(int n) { return (n + GA_ROWS - 1) / GA_ROWS; }
+int64_t ga_halves(int n) { return (n + GA_ROWS / 2 - 1) / (GA_ROWS / 2); }
 bool ga_fine(const GroupedArgs& a) {
-  return (int64_t)a.batch * a.q_heads * a.n_q <= (1 << 16) / a.n_k;
+  const int64_t heads = (int64_t)a.batch * a.q_heads;
+  return heads * a.n_q <= (1 << 16) / a.n_k && heads * ga_tiles(a.n_q) <= GA_FINE_BLOCKS;
 }
 
 // Whether blocks of 128 queries are so few that a CU is better given blocks of 64
@@ -1024,13 +1028,10 @@ bool ga_fine(const GroupedArgs& a) {
 // 24.0 + 96.3; 256 x 1 of 1000 42.6 + 116, 44.6 + 151; 35 x 3 of 237 of 128, 8 over 4
 // 9.5 + 28.3, 7.8 + 34.6.
 bool ga_few(const GroupedArgs& a, int64_t blocks) {
-  if (ga_fine(a)) return blocks <= GA_FINE_BLOCKS;
-  return blocks <= (a.causal && a.n_q >= 768 ? 256 : a.n_q <= 64 && a.n_k >= 1024 ? 512 : 128);
+  return ga_fine(a) || blocks <= (a.causal && a.n_q >= 768 ? 256 : a.n_q <= 64 && a.n_k >= 1024 ? 512 : 128);
 }
 // As many sets as the tiles leave LDS for, two blocks to a CU with head dimension 128.
 constexpr int ga_sets(int D) { return D == 64 ? 4 : 2; }
-int64_t ga_tiles(int n) { return (n + GA_ROWS - 1) / GA_ROWS; }
-int64_t ga_halves(int n) { return (n + GA_ROWS / 2 - 1) / (GA_ROWS / 2); }
 
 template <int D>
 hipError_t ga_forward(const GroupedArgs& a, hipStream_t st) {
@@ -1101,10 +1102,10 @@ hipError_t ga_backward(const GroupedArgs& a, hipStream_t st) {
       // by two; 4 x 500: 28.0, 27.0; but 20 x 500, 64 steps: 43.5, 48.3).
       const int halves = (int)(nb * ga_halves(a.n_k) * a.kv_heads * a.parts);
       const int64_t steps = (int64_t)(a.n_q + GA_STEP - 1) / GA_STEP * a.group / a.parts;
-      if (nb * kv > 256)
-        ga_bwd_kv_kernel<4, 1><<<(int)(nb * kv), 256, 0, st>>>(s);
-      else if (fine)
+      if (fine)
         ga_bwd_kv_kernel<2, 2, true><<<halves, 256, 0, st>>>(s);
+      else if (nb * kv > 256)
+        ga_bwd_kv_kernel<4, 1><<<(int)(nb * kv), 256, 0, st>>>(s);
       else if (steps <= 32)
         ga_bwd_kv_kernel<2, 2><<<halves, 256, 0, st>>>(s);
       else

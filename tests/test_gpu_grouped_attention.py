@@ -324,3 +324,18 @@ def test_few_scores_of_many_keys_are_as_near(case):
             err = np.linalg.norm(host(g) - r)
             print(f"  {name}: {err / own:.3f} of its own rounding", flush=True)
             assert err <= 1.05 * own, name
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_few_scores_over_more_key_tiles_than_compute_units(hd):
+    """One query of 40000 keys: 313 tiles of keys, and all gradients as near as of fewer."""
+    q, k, v, do = draw(1, 1, 40000, 1, 1, hd, seed=1, size=3.0)
+    out, lse = hcmix.grouped_attention_forward(q, k, v)
+    got = (out, *hcmix.grouped_attention_backward(q, k, v, out, lse, do))
+    hq, hk, hv, hdo = (host(t) for t in (q, k, v, do))
+    ref = (grouped.forward(hq, hk, hv)[0], *grouped.backward(hq, hk, hv, hdo)[0])
+    for name, g, r in zip(("out", "dq", "dk", "dv"), got, ref):
+        own = np.linalg.norm(host(torch.from_numpy(r).to(torch.bfloat16)) - r)
+        err = np.linalg.norm(host(g) - r)
+        print(f"  {name}: {err / own:.3f} of its own rounding", flush=True)
+        assert err <= 1.05 * own, name
