@@ -100,3 +100,27 @@ def test_a_million_sequences_of_one_position():
     assert torch.equal(dv, do)
     limit = 4 * 2.0 ** -24 * 128 * 6 * 6 * 6 * hd ** -0.5
     assert max(dq.abs().max().item(), dk.abs().max().item()) <= limit
+
+
+@pytest.mark.parametrize("n_k", [70, 300])
+def test_key_gradients_of_the_last_of_a_million_queries(n_k):
+    """The key gradients where only the last 50 queries' outputs have a gradient (all
+    others add zeros): those queries' own, element by element, from rows past 2^31
+    elements."""
+    n, heads, hd = 1 << 20, 33, 64
+    g = torch.Generator("cuda").manual_seed(3)
+    q = torch.randn((1, n, heads, hd), generator=g, device="cuda", dtype=torch.bfloat16)
+    assert q.numel() > 1 << 31
+    k, v = (torch.randn((1, n_k, heads, hd), generator=g, device="cuda", dtype=torch.bfloat16)
+            for _ in range(2))
+    do = torch.zeros_like(q)
+    s = slice(n - 50, n)
+    do[:, s] = torch.randn((1, 50, heads, hd), generator=g, device="cuda", dtype=torch.bfloat16)
+    out, lse = hcmix.grouped_attention_forward(q, k, v, causal=False)
+    got = hcmix.grouped_attention_backward(q, k, v, out, lse, do, causal=False)
+    assert not got[0][:, :n - 50].any()
+    ref, bounds = grouped.backward(host(q[:, s]), host(k), host(v), host(do[:, s]), causal=False)
+    for name, t, r, b in zip(("dq", "dk", "dv"), (got[0][:, s], *got[1:]), ref, bounds):
+        err = np.abs(host(t) - r)
+        print(f"  {name}: largest error {err.max():.2e}, of its bound {(err / b).max():.2f}", flush=True)
+        assert (err <= b).all(), name
