@@ -144,7 +144,7 @@ class HybridStack:
             gs += gout
             codes += [c for _, c in arg]
             order += [j for j, _ in arg]
-        dws, dwo = hcmix.stack_weight_gradients(xs, gs, codes, self.causal)
+        dws, dwo = hcmix.stack_weight_gradients(xs, gs, codes, self.causal) if xs else ([], [])
         self.dw_self = [None] * self.num_sparse
         self.dw_off = [None] * self.num_sparse
         for k, j in enumerate(order):

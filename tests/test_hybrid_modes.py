@@ -59,3 +59,14 @@ def test_attention_layers_take_the_stacks_direction(calls, n, kv, causal, want):
     h._dw_in, h.dw_attn = [], [None]
     h.backward_segment(0, torch.ones_like(y))
     assert calls == [want, want]
+
+
+def test_a_stack_of_attention_layers_alone_has_a_backward(calls):
+    g = torch.Generator().manual_seed(1)
+    attn = [(torch.randn((6 * 64, 64), generator=g).to(torch.bfloat16),
+             torch.randn((64, 128), generator=g).to(torch.bfloat16)) for _ in range(2)]
+    h = HybridStack(["attn", "attn"], [], [], attn, 2)
+    x = torch.randn((2, 32, 64), generator=g).to(torch.bfloat16)
+    dx = h.backward(torch.ones_like(h.forward(x)))
+    assert dx.shape == x.shape and h.dw_self == [] and h.dw_off == []
+    assert [[w.shape for w in p] for p in h.dw_attn] == [[(384, 64), (64, 128)]] * 2
