@@ -216,7 +216,11 @@ class HybridDecoder:
                 continue
             wqkv, wout, hd, cache, xin, qkv, o = part
             if batch % 2:
-                xin[:batch].copy_(x)
+                own = xin[:batch]
+                if x.shape != own.shape or x.dtype != own.dtype:     # copy_ would make it fit
+                    raise ValueError(f"x: shape {tuple(x.shape)} and dtype {x.dtype}, expected "
+                                     f"{tuple(own.shape)} and {own.dtype}")
+                own.copy_(x)
                 x = xin
             hcmix.linear_forward(x, wqkv, out=qkv)
             packed = qkv[:batch].view(batch, 1, -1, hd)

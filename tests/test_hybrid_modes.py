@@ -70,3 +70,17 @@ def test_a_stack_of_attention_layers_alone_has_a_backward(calls):
     dx = h.backward(torch.ones_like(h.forward(x)))
     assert dx.shape == x.shape and h.dw_self == [] and h.dw_off == []
     assert [[w.shape for w in p] for p in h.dw_attn] == [[(384, 64), (64, 128)]] * 2
+
+
+@pytest.mark.parametrize("batch", [2, 3])
+def test_a_decoder_takes_its_own_batch(batch):
+    """An odd batch is copied into rows of the decoder's own: one row of x is not given
+    to every window, nor another type converted."""
+    attn = (torch.zeros((6 * 64, 64), dtype=torch.bfloat16), torch.zeros((64, 128), dtype=torch.bfloat16))
+    d = HybridStack(["attn"], [], [], [attn], 2).decoder(batch, 16, "cpu")
+    bf = torch.bfloat16
+    for x, match in ((torch.zeros((1, 64), dtype=bf), "shape"), (torch.zeros(64, dtype=bf), "shape"),
+                     (torch.zeros((batch, 1), dtype=bf), "shape"),
+                     (torch.zeros((batch, 64)), "dtype"), (torch.zeros((batch, 64), dtype=bf), "GPU")):
+        with pytest.raises(ValueError, match=match):
+            d.step(x, 0)
