@@ -587,7 +587,9 @@ hcmix_status hcmix_rotary(int64_t rows, int32_t heads, int32_t head_dim, int32_t
  * Precision: products of bf16 with fp32 accumulation, softmax statistics in fp32,
  * P (and the backward's P and dS) rounded to bf16 for the second products, or taken
  * as two bf16 numbers in a call of at most 2^16 scores (batch q_heads n_q n_k) in at
- * most 256 blocks of 128 queries of a head (batch q_heads ceil(n_q / 128)).
+ * most 256 blocks of 128 queries of a head (batch q_heads ceil(n_q / 128)).  P v is
+ * summed with P up to 2^8 before it is divided by their sum: values have to stay below
+ * 2^120 / n_k for that to stay in 32 bits.
  * n_q, n_k <= 2^20, q_heads <= 1024, batch * n <= 2^30; scale 2^-24 .. 2^24.
  * HCMIX_ERR_INVALID_VALUE: null pointers (lengths may be), sizes < 1 or past
  * those bounds, q_heads no multiple of kv_heads, causal not 0 or 1, strides
@@ -604,6 +606,8 @@ hcmix_status hcmix_grouped_attention_forward(
  * its out and lse, and dout = dL/dout (contiguous like out):
  *   dv = P^T dout, dS = P * (dout v^T - rowsum(dout * out)) scale,
  *   dq = dS k, dk = dS^T q, summed over the query heads of a group.
+ * rowsum(dout * out) is taken as rowsum(P * dout v^T) in rows that see at most 128 keys
+ * and in the calls of few scores named above, in others from out as bf16 has it.
  * P is made again from lse.  Sums run in a fixed order (bitwise-repeatable).
  * q, out and dout have to be finite in every row, those that see nothing among
  * them (their weight of 0 meets them).
@@ -650,8 +654,10 @@ hcmix_status hcmix_grouped_attention_backward(
  * Attention: `tokens` queries of every sequence, the last standing at its last
  * token: query t at position lengths[b] - tokens + t sees the tokens up to its
  * own.  q bf16 [batch][tokens][q_heads][head_dim], rows q_stride apart; out bf16,
- * contiguous; softmax, groups and precision as for hcmix_grouped_attention, keys
- * and values exact.  A query before the first token gets 0.  lengths: int32
+ * contiguous; softmax, groups and precision as for hcmix_grouped_attention (one bf16
+ * number for P, which is at most 1: values below 2^128 / length), keys and values exact.
+ * Values held up to lengths[b] have to be finite also where a query is before them (a
+ * weight of 0 meets them).  A query before the first token gets 0.  lengths: int32
  * [batch], taken within 0 .. capacity.  max_length (1 .. capacity) says how long
  * sequences are expected to be: long ones are split over the chip by it (joined
  * through the workspace of hcmix_kv_cache_attention_workspace_bytes, possibly 0;

@@ -57,10 +57,11 @@ __device__ __forceinline__ bf16x8 ga_trfrag(const bf16* t, int k0, int c0, int l
 // What att_pack's rounding leaves of those registers, rounded in its turn.  In a call
 // of few scores the roundings of P and dS do not average out: of 1024 and fewer, dq
 // and dk were up to 1.5 to 2.8 times as far off as their own rounding to bf16 leaves
-// them, 1.42 in the mean; from 131072 on 1.45 at most.  Such a call waits for
-// latencies, so that the FINE kernels' second products with what is left cost it
-// little (1 x 128, 2 heads of 64: 5.2 + 14.1 us, 5.4 + 16.5), and its results are as
-// near as their own rounding.
+// them, 1.42 in the mean; from 131072 on 1.45 at most (scores of order 1).  Such a call
+// waits for latencies, so that the FINE kernels' second products with what is left, and
+// what they take for D, cost it less than they compute (1 x 128, 2 heads of 64 5.2 + 12.7
+// us, 5.4 + 14.6; 1 x 16 of 512, 4 heads of 128 9.0 + 18.7, 10.3 + 23.5), and its results
+// are as near as their own rounding.
 __device__ __forceinline__ bf16x8 ga_rest(const f32x16& s, int m) {
   bf16x8 v;
 #pragma unroll
@@ -1006,8 +1007,8 @@ constexpr int64_t GA_MAX_BLOCKS = 1 << 22;     // of a launch, up to 512 threads
 
 // Whether the scores of a call are so few that their roundings do not average
 // (ga_rest), for all of its kernels alike.  Such calls are given the form for few blocks,
-// up to so many blocks of 128 queries: it costs 100 x 8 positions, 2 heads of 64 3.8 + 9.7
-// us, 5.2 + 10.7 so, but 512 x 4 5.7 + 15.4, 10.6 + 28.0, and so many sequences' roundings
+// up to so many blocks of 128 queries: it costs 100 x 8 positions, 2 heads of 64 3.8 + 9.2
+// us, 5.2 + 11.1 so, but 512 x 4 5.6 + 15.4, 10.4 + 31.1, and so many sequences' roundings
 // nearly average.
 constexpr int64_t GA_FINE_BLOCKS = 256;
 int64_t ga_tiles(int n) { return (n + GA_ROWS - 1) / GA_ROWS; }

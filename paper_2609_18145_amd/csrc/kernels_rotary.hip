@@ -144,7 +144,8 @@ hipError_t launch_rotary(RotaryArgs a, int layout_half, int elem_bytes, hipStrea
   a.all_magic = ((1ull << 44) + all - 1) / all;
   // Rows to a block: more share the wait for the angles, fewer leave more blocks
   // to hide it: 8 x 4096 positions, 20 heads of 64 (168 MB): 36.9 us with 16 and 8,
-  // 34.0 with 4 (4.9 TB/s; a copy of as much takes 33.7).  With few heads more, up
+  // 34.2 with 4 (4.9 TB/s; a copy of as much takes 33.8; the same tensors again and again,
+  // which the Infinity Cache partly holds, 25.9, a copy 24.2).  With few heads more, up
   // to a unit for every thread: 64 x 2048, 2 heads of 64 31.0 us with 4, 20.5; 4 heads
   // 40.2, 29.0; 2 of 20, by single values, 29.7, 16.6.
   int rpb = 1;
