@@ -18,7 +18,8 @@
 // keys: kv_slot puts a lane's 16 keys of the block in 16 consecutive bytes of
 // each dimension's row.  So both operands go from memory to registers to the
 // matrix instruction, with no LDS and no transposition, in 16-byte loads of
-// whole lines; the conversion to bf16 multiplies the scale in, exactly.
+// whole lines; the conversion to bf16 multiplies the scale in, exactly.  P, the other
+// operand of that instruction, is rounded to bf16 as well; its sum is taken before.
 #include <algorithm>
 
 #include "hcmix_internal.h"

@@ -6,7 +6,8 @@
 // head's first rot_dim values; the others are copied.  The inverse takes -t: it
 // is the transpose, hence also the backward.
 //
-// The angle is taken in 64 bits, in turns, and only its fraction is rounded: a
+// The angle is taken in 64 bits, in turns, and only its fraction is rounded, by 2^-22.3
+// radians at most (fp32 results 5.1e-8 off in norm, where 64-bit sines leave 3.8e-8): a
 // position of 10^6 times a frequency in 32 bits is off by 0.06 radians.  Every
 // head of a position shares the angles, so a block first makes the table of its
 // rows' (cos, sin) in LDS and then streams the heads past it: bound by memory, at
