@@ -339,3 +339,21 @@ def test_few_scores_over_more_key_tiles_than_compute_units(hd):
         err = np.linalg.norm(host(g) - r)
         print(f"  {name}: {err / own:.3f} of its own rounding", flush=True)
         assert err <= 1.05 * own, name
+
+
+@pytest.mark.parametrize("case", [(1, 200, 150, 2, 1, 64, None), (1, 200, 150, 2, 1, 128, None), (2, 100, 160, 2, 2, 64, [131, 0]),
+                                  (2, 100, 160, 2, 1, 128, [160, 140]), (40, 260, 200, 4, 2, 64, None),
+                                  (40, 260, 200, 4, 4, 128, None)], ids=lambda c: "x".join(map(str, c[:6])))
+def test_blocks_of_empty_short_and_long_rows(case):
+    """Rows that see nothing, at most 128 keys and more beside each other, in calls of few
+    scores and of many."""
+    print(f"case: grouped attention {case}", flush=True)
+    batch, n_q, n_k, heads, kv, hd, lengths = case
+    q, k, v, do = draw(batch, n_q, n_k, heads, kv, hd, seed=n_q, size=3.0)
+    check(q, k, v, do, True, lengths)
+    ln = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    out, lse = hcmix.grouped_attention_forward(q, k, v, True, ln)
+    dq, dk, _ = hcmix.grouped_attention_backward(q, k, v, out, lse, do, True, ln)
+    ref, bounds = grouped.backward(*(host(t) for t in (q, k, v, do)), True, lengths, exact=128)
+    within("dq", dq, ref[0], bounds[0])
+    within("dk", dk, ref[1], bounds[1])
